@@ -51,9 +51,10 @@ typedef enum {
 enum { CERBERUS_F32 = 0, CERBERUS_BF16 = 1 };
 
 /* bits of cerberus_state.status (device word) */
-enum { CERBERUS_DEV_KV_OVERFLOW = 1, CERBERUS_DEV_BAD_TOKEN = 2, CERBERUS_DEV_LOG_FULL = 4 };
+enum { CERBERUS_DEV_KV_OVERFLOW = 1, CERBERUS_DEV_BAD_TOKEN = 2, CERBERUS_DEV_LOG_FULL = 4, CERBERUS_DEV_BAD_PAGE = 8 };
 
-enum { CERBERUS_MAX_TREE = 192, CERBERUS_MAX_HEADS = 8, CERBERUS_MAX_TOPK = 16, CERBERUS_MAX_BATCH = 16 };
+enum { CERBERUS_MAX_TREE = 192, CERBERUS_MAX_HEADS = 8, CERBERUS_MAX_TOPK = 16, CERBERUS_MAX_BATCH = 16,
+       CERBERUS_MAX_SEQS = 1024 /* sequences of a page table */ };
 
 /* Model and method parameters (Algorithm 1 "Require": N layers, threshold T; Section 5.1
  * "Training": 4 heads of 4 Resblocks + 1 FC).                                                 */
@@ -195,6 +196,90 @@ int cerberus_accept(cerberus_ctx *ctx, const int32_t *node_argmax, const int32_t
  * The array's address is resolved by cerberus_init on the context's device.                    */
 int cerberus_accept_noalloc(cerberus_ctx *ctx, const int32_t *node_argmax, const int32_t *node_token,
                             const cerberus_state *st, int32_t batch, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A key-value cache in pages.  The slab of cerberus_state reserves kv_capacity rows for every sequence; here sequences
+ * share a pool of pages and hold as many as their length needs.  A page is page_size rows (a power of two, 16..256) of every
+ * key head; row r of a sequence lies in block r / page_size of its block table, at offset r % page_size of that page.  The calls
+ * below need no context; they run on the device that is current, allocate nothing and may be captured into a graph.
+ * One layer's pages and the tables (which all layers share):                                     */
+typedef struct {
+  void *k, *v;            /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned     */
+  void *bounds;           /* DEVICE [n_pages][n_kv_heads][2][head_dim]: lowest and highest coordinate of the keys that the page
+                             holds, for cerberus_page_select; may be NULL                        */
+  int32_t n_pages, page_size, n_kv_heads;
+  int32_t head_dim;       /* 64 or 128                                                           */
+  int32_t dtype;          /* CERBERUS_F32 or CERBERUS_BF16: of pages, bounds, rows, queries and outputs */
+} cerberus_pages;
+
+typedef struct {
+  int32_t *block_table;   /* DEVICE [max_seqs][max_blocks] page of every block                     */
+  int32_t *kv_len;        /* DEVICE [max_seqs] rows that the sequence holds                        */
+  int32_t *free_pages;    /* DEVICE [n_pages]; the first *n_free are the free pages, taken from the end */
+  int32_t *n_free;        /* DEVICE, one word                                                     */
+  int32_t *status;        /* DEVICE, one sticky word, OR of CERBERUS_DEV_* bits                    */
+  int32_t max_seqs;       /* 1..CERBERUS_MAX_SEQS                                                */
+  int32_t max_blocks, page_size, n_pages;   /* max_blocks * page_size and n_pages * page_size below 2^31 */
+} cerberus_page_table;
+
+/* Gives the next rows of sequences 0..batch-1 their places, in order of the sequences.  new_rows (DEVICE [batch]): rows that
+ * sequence b is to grow by, 0 for none; below 0 the sequence ends: its pages go back to the free pages (to be had by this
+ * call's other sequences already) and kv_len[b] becomes 0.  row_start (DEVICE [batch + 1]): sequence b's rows are rows
+ * row_start[b] .. of the batch, refused ones counted like others (2^31 - 1 where the sum
+ * is more).  slot (DEVICE [max_rows]): page * page_size + offset
+ * of every row, -1 for rows of refused sequences and behind the last row.  first_pos (DEVICE [batch]): rows that the
+ * sequence held before, -1 where it ended or was refused.  kv_len and the block tables are those with the new rows.
+ * A sequence is refused (CERBERUS_DEV_KV_OVERFLOW; it keeps what it has) if its table or max_rows has no room for its
+ * rows, or if it needs pages and those that it and the sequences before it need are more than there are: first come,
+ * first served.  A kv_len that no table can hold counts as no room, and such a sequence ends without returning pages.   */
+int cerberus_page_plan(const cerberus_page_table *pt, const int32_t *new_rows, int32_t batch, int32_t max_rows,
+                       int32_t *row_start, int32_t *first_pos, int32_t *slot, void *stream);
+
+/* Writes n_rows rows of K and V (DEVICE, row i of head h at k + i * k_row_stride + h * k_head_stride elements, head_dim of
+ * them contiguous; addresses and strides multiples of 16 bytes) into their slots; rows with a slot below 0 are skipped, rows
+ * whose slot lies outside the pages too (CERBERUS_DEV_BAD_PAGE in *status, DEVICE, may be NULL).  Where pg->bounds is set, the bounds of
+ * every page written to become those of its rows up to the last one written.  For that the rows of one call that share
+ * a page have to be consecutive and in order (as cerberus_page_plan places them), and the rows before them in the page
+ * stored already.  No two rows of a call may have the same slot.                                */
+int cerberus_page_store(const cerberus_pages *pg, const void *k, int64_t k_row_stride, int64_t k_head_stride, const void *v,
+                        int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot, int32_t n_rows, int32_t *status,
+                        void *stream);
+
+/* Bytes of DEVICE workspace (256-byte aligned) that cerberus_page_select, cerberus_paged_attention or, with the pages of a
+ * context's layers, cerberus_paged_step need for such a call; 0 on bad input.  n_select 0: no selection.  Calls that share
+ * a workspace must not overlap.                                                                 */
+size_t cerberus_paged_workspace_bytes(const cerberus_pages *pg, const cerberus_page_table *pt, int32_t batch, int32_t n_heads,
+                                      int32_t n_select);
+
+/* Chooses blocks to attend to.  q: DEVICE, query of head h of sequence b at q + b * q_row_stride + h * head_dim elements
+ * (16-byte aligned); n_heads a multiple of n_kv_heads, consecutive heads share a key head.  With Q the sum of the queries of
+ * a key head, block j scores sum_d Q_d * (Q_d >= 0 ? highest_d : lowest_d), no less than the sum of its group's scores on any
+ * one key of the block.  Per sequence and key head the newest block, then the first one, then those with the highest scores
+ * (summed in 64 bits; NaN counts as the highest; ties: the lower index) up to n_select are written to blocks (DEVICE
+ * [batch][n_kv_heads][n_select]) in ascending order, the rest -1.  Needs pg->bounds.            */
+int cerberus_page_select(const cerberus_pages *pg, const cerberus_page_table *pt, const void *q, int64_t q_row_stride,
+                         int32_t batch, int32_t n_heads, int32_t n_select, int32_t *blocks, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* Attention of one new token per sequence: out = softmax(scale * q K^T) V over rows 0..kv_len[b]-1 (the token's own row is
+ * stored already), out laid out like q with a row stride of its own.  With blocks (as cerberus_page_select writes them, in any order; an index twice counts
+ * twice; indexes outside 0..blocks held - 1 are no block) each key head reads those blocks only.  Where there is no row to
+ * read, or every score is -inf, the output is zero.  What lies in a page behind the last row is never used.  A kv_len above what the table holds
+ * counts as that, a page number outside the pool as no rows (CERBERUS_DEV_BAD_PAGE, pt->status).  fp32 softmax and sums; bf16
+ * probabilities are two bf16 planes.                                                            */
+int cerberus_paged_attention(const cerberus_pages *pg, const cerberus_page_table *pt, const void *q, int64_t q_row_stride,
+                             void *out, int64_t out_row_stride, int32_t batch, int32_t n_heads, float scale,
+                             const int32_t *blocks, int32_t n_select, void *workspace, size_t workspace_bytes, void *stream);
+
+/* cerberus_ar_step with the cache in pages: layers (HOST [n_layers]) are the pages of every layer (all of one shape: the model's heads, its
+ * head_dim and dtype).  new_rows (DEVICE [batch], NULL: 1 for all): 1 the sequence decodes a token, 0 it sits the step
+ * out, below 0 it ends.  A sequence without room for its row sits out too (CERBERUS_DEV_KV_OVERFLOW in pt->status).
+ * n_select > 0: every layer attends to that many blocks, chosen per layer (needs bounds).  st as in cerberus_ar_step, but
+ * st->kv and st->kv_len are not used; the rows are counted in pt->kv_len.  In bf16 mode the token's own row is attended to as
+ * the cache holds it, in bf16.                                                                  */
+int cerberus_paged_step(cerberus_ctx *ctx, const cerberus_state *st, const cerberus_pages *layers, const cerberus_page_table *pt,
+                        int32_t batch, const int32_t *new_rows, int32_t n_select, void *workspace, size_t workspace_bytes,
+                        void *stream);
 
 /* Installs (or, with NULL, clears) the taps; the struct is copied.                             */
 int cerberus_set_taps(cerberus_ctx *ctx, const cerberus_taps *taps);

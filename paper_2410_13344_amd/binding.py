@@ -14,8 +14,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcerberus.so")
 
 CERBERUS_F32, CERBERUS_BF16 = 0, 1
-CERBERUS_DEV_KV_OVERFLOW, CERBERUS_DEV_BAD_TOKEN, CERBERUS_DEV_LOG_FULL = 1, 2, 4   # bits of the device status word
+CERBERUS_DEV_KV_OVERFLOW, CERBERUS_DEV_BAD_TOKEN, CERBERUS_DEV_LOG_FULL, CERBERUS_DEV_BAD_PAGE = 1, 2, 4, 8   # bits of the device status word
 CERBERUS_MAX_TREE, CERBERUS_MAX_HEADS, CERBERUS_MAX_TOPK, CERBERUS_MAX_BATCH = 192, 8, 16, 16
+CERBERUS_MAX_SEQS = 1024
 DEV_KV_OVERFLOW, DEV_BAD_TOKEN = 1, 2
 
 c_i32p = C.POINTER(C.c_int32)
@@ -53,6 +54,16 @@ class Taps(C.Structure):
                 ("forced_gate_hidden", C.c_void_p)]
 
 
+class Pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("bounds", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class PageTable(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("block_table", "kv_len", "free_pages", "n_free", "status")] + [
+        (n, C.c_int32) for n in ("max_seqs", "max_blocks", "page_size", "n_pages")]
+
+
 _lib = None
 
 
@@ -84,6 +95,19 @@ def lib() -> C.CDLL:
         L.cerberus_accept.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(State), C.c_int32, C.c_void_p]
         L.cerberus_accept_noalloc.restype = C.c_int
         L.cerberus_accept_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(State), C.c_int32, C.c_void_p]
+        pages, table, i32, i64, vp = C.POINTER(Pages), C.POINTER(PageTable), C.c_int32, C.c_int64, C.c_void_p
+        L.cerberus_page_plan.restype = C.c_int
+        L.cerberus_page_plan.argtypes = [table, vp, i32, i32, vp, vp, vp, vp]
+        L.cerberus_page_store.restype = C.c_int
+        L.cerberus_page_store.argtypes = [pages, vp, i64, i64, vp, i64, i64, vp, i32, vp, vp]
+        L.cerberus_paged_workspace_bytes.restype = C.c_size_t
+        L.cerberus_paged_workspace_bytes.argtypes = [pages, table, i32, i32, i32]
+        L.cerberus_page_select.restype = C.c_int
+        L.cerberus_page_select.argtypes = [pages, table, vp, i64, i32, i32, i32, vp, vp, C.c_size_t, vp]
+        L.cerberus_paged_attention.restype = C.c_int
+        L.cerberus_paged_attention.argtypes = [pages, table, vp, i64, vp, i64, i32, i32, C.c_float, vp, i32, vp, C.c_size_t, vp]
+        L.cerberus_paged_step.restype = C.c_int
+        L.cerberus_paged_step.argtypes = [C.c_void_p, C.POINTER(State), pages, table, i32, vp, i32, vp, C.c_size_t, vp]
         L.cerberus_set_taps.restype = C.c_int
         L.cerberus_set_taps.argtypes = [C.c_void_p, C.POINTER(Taps)]
         L.cerberus_set_param.restype = C.c_int
@@ -210,6 +234,41 @@ def cerberus_accept_noalloc(ctx: int, node_argmax: torch.Tensor, node_token: tor
                                          _stream_ptr(stream)))
 
 
+def cerberus_page_plan(table: PageTable, new_rows: torch.Tensor, max_rows: int, row_start: torch.Tensor, first_pos: torch.Tensor,
+                       slot: torch.Tensor, stream=None) -> None:
+    _check(lib().cerberus_page_plan(table, new_rows.data_ptr(), new_rows.shape[0], max_rows, row_start.data_ptr(),
+                                    first_pos.data_ptr(), slot.data_ptr(), _stream_ptr(stream)))
+
+
+def cerberus_page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, status: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    _check(lib().cerberus_page_store(pages, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                     slot.data_ptr(), slot.shape[0], _ptr(status), _stream_ptr(stream)))
+
+
+def cerberus_paged_workspace_bytes(pages: Pages, table: PageTable, batch: int, n_heads: int, n_select: int = 0) -> int:
+    return int(lib().cerberus_paged_workspace_bytes(pages, table, batch, n_heads, n_select))
+
+
+def cerberus_page_select(pages: Pages, table: PageTable, q: torch.Tensor, blocks: torch.Tensor, workspace: torch.Tensor,
+                         stream=None) -> None:
+    _check(lib().cerberus_page_select(pages, table, q.data_ptr(), q.stride(0), q.shape[0], q.shape[1], blocks.shape[2],
+                                      blocks.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+
+
+def cerberus_paged_attention(pages: Pages, table: PageTable, q: torch.Tensor, out: torch.Tensor, scale: float,
+                             blocks: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    _check(lib().cerberus_paged_attention(pages, table, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), q.shape[0], q.shape[1],
+                                          scale, _ptr(blocks), 0 if blocks is None else blocks.shape[2], workspace.data_ptr(),
+                                          workspace.numel(), _stream_ptr(stream)))
+
+
+def cerberus_paged_step(ctx: int, state: State, layers, table: PageTable, batch: int, new_rows: Optional[torch.Tensor], n_select: int,
+                        workspace: torch.Tensor, stream=None) -> None:
+    _check(lib().cerberus_paged_step(ctx, C.byref(state), layers, table, batch, _ptr(new_rows), n_select, workspace.data_ptr(),
+                                     workspace.numel(), _stream_ptr(stream)))
+
+
 def cerberus_set_taps(ctx: int, taps: Optional[Taps]) -> None:
     _check(lib().cerberus_set_taps(ctx, C.byref(taps) if taps is not None else None))
 
@@ -269,6 +328,157 @@ class DeviceTaps:
         self.struct = Taps(*[_ptr(getattr(self, n)) for n, _ in Taps._fields_])
 
 
+class PagePlan:
+    """Where a batch's new rows go (see cerberus_page_plan)."""
+
+    def __init__(self, batch: int, max_rows: int, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.max_rows = max_rows
+        self.row_start = torch.zeros(batch + 1, **i32)
+        self.first_pos = torch.zeros(batch, **i32)
+        self.slot = torch.full((max(max_rows, 1),), -1, **i32)
+
+
+class PageCache:
+    """A key-value cache in pages that up to max_seqs sequences share: the device arrays of a cerberus_page_table and of the
+    cerberus_pages of n_layers layers, and the workspace of the calls on them.  max_blocks: blocks of a sequence at most.  The
+    bookkeeping (free pages, status, lengths, tables) is one tensor, `words`: a copy of it is a snapshot of who owns which page.
+    A call on another stream than torch's current one of the cache's device: pass it as `stream`, and order the streams as for
+    any tensor.  Outputs and workspaces come from torch's allocator per call, on the call's stream, so calls on
+    several streams, and captured graphs, do not share them."""
+
+    def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int, max_seqs: int,
+                 max_blocks: int, bounds: bool = True, device="cuda"):
+        if dtype not in (CERBERUS_F32, CERBERUS_BF16):
+            raise ValueError("dtype must be CERBERUS_F32 or CERBERUS_BF16")
+        if min(n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_blocks) < 1 or n_layers < 0:
+            raise ValueError("non-positive size of a page cache")
+        self.dtype = torch.float32 if dtype == CERBERUS_F32 else torch.bfloat16
+        self.device = torch.device(device, torch.cuda.current_device()) if torch.device(device).index is None else torch.device(device)
+        self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_layers, n_pages, page_size, n_kv_heads, head_dim
+        self.max_seqs, self.max_blocks = max_seqs, max_blocks
+        shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        self.k = torch.zeros(shape, dtype=self.dtype, device=device)
+        self.v = torch.zeros(shape, dtype=self.dtype, device=device)
+        self.bounds = torch.zeros((n_layers, n_pages, n_kv_heads, 2, head_dim), dtype=self.dtype, device=device) if bounds else None
+        self.words = torch.zeros(2 + max_seqs + n_pages + max_seqs * max_blocks, dtype=torch.int32, device=device)
+        at = 2 + max_seqs
+        self.n_free, self.status, self.kv_len = self.words[0:1], self.words[1:2], self.words[2:at]
+        self.free_pages = self.words[at:at + n_pages]
+        self.block_table = self.words[at + n_pages:].view(max_seqs, max_blocks)
+        self.n_free.fill_(n_pages)
+        self.free_pages.copy_(torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device))   # page 0 is taken first
+        self.table = PageTable(*[getattr(self, n).data_ptr() for n in ("block_table", "kv_len", "free_pages", "n_free", "status")],
+                               max_seqs, max_blocks, page_size, n_pages)
+        self.layers = (Pages * max(n_layers, 1))()
+        for i in range(n_layers):
+            self.layers[i] = Pages(self.k[i].data_ptr(), self.v[i].data_ptr(), self.bounds[i].data_ptr() if bounds else None,
+                                   n_pages, page_size, n_kv_heads, head_dim, dtype)
+        self._bytes = {}
+
+    def new_plan(self, batch: int, max_rows: int) -> PagePlan:
+        return PagePlan(batch, max_rows, self.device)
+
+    def workspace_bytes(self, batch: int, n_heads: int, n_select: int = 0) -> int:
+        key = (batch, n_heads, n_select)
+        n = self._bytes.get(key)
+        if n is None:
+            n = cerberus_paged_workspace_bytes(self._layer(0), self.table, batch, n_heads, n_select)
+            if n == 0:
+                raise CerberusError(-2)
+            self._bytes[key] = n
+        return n
+
+    def _on(self, stream):
+        """Makes the cache's device and the call's stream torch's current ones."""
+        return torch.cuda.stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+
+    def _is(self, what: str, t: torch.Tensor, dtype, shape) -> None:
+        if t.dtype != dtype or t.device != self.device or t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
+            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {shape} on {self.device}")
+
+    def plan(self, new_rows: torch.Tensor, max_rows: Optional[int] = None, out: Optional[PagePlan] = None, stream=None) -> PagePlan:
+        """Places for the next rows of sequences 0..len(new_rows)-1.  max_rows: room of the slot map (with `out`: that plan's)."""
+        self._is("new_rows", new_rows, torch.int32, (None,))
+        batch = new_rows.shape[0]
+        if not new_rows.is_contiguous():
+            raise ValueError("new_rows must be contiguous")
+        with self._on(stream):
+            if out is None:
+                if max_rows is None:
+                    raise ValueError("plan needs max_rows or out")
+                out = PagePlan(batch, max_rows, self.device)
+            elif out.first_pos.shape[0] != batch or out.first_pos.device != self.device or (max_rows is not None and max_rows != out.max_rows):
+                raise ValueError("out is a plan of another batch, device or max_rows")
+            cerberus_page_plan(self.table, new_rows, out.max_rows, out.row_start, out.first_pos, out.slot)
+        return out
+
+    def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, stream=None) -> None:
+        """Rows k, v [rows][n_kv_heads][head_dim] (any strides of rows and heads) into their slots."""
+        self._is("slot", slot, torch.int32, (None,))
+        shape = (slot.shape[0], self.n_kv_heads, self.head_dim)
+        self._is("k", k, self.dtype, shape)
+        self._is("v", v, self.dtype, shape)
+        pages = self._layer(layer)
+        if shape[0] == 0:
+            return
+        if k.stride(2) != 1 or v.stride(2) != 1 or not slot.is_contiguous():
+            raise ValueError("a row of k and v, and slot, must be contiguous")
+        with self._on(stream):
+            cerberus_page_store(pages, k, v, slot, self.status)
+
+    def _layer(self, layer: int) -> Pages:
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer {layer} out of 0..{self.n_layers - 1}")
+        return self.layers[layer]
+
+    def _query(self, what: str, q: torch.Tensor) -> None:
+        self._is(what, q, self.dtype, (None, None, self.head_dim))
+        if q.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != self.head_dim):
+            raise ValueError(f"the heads of a row of {what} must be contiguous")
+
+    def select(self, layer: int, q: torch.Tensor, n_select: int, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The n_select blocks of every sequence and key head that q [batch][n_heads][head_dim] attends to."""
+        self._query("q", q)
+        pages = self._layer(layer)
+        if not 1 <= n_select <= self.max_blocks:
+            raise ValueError(f"n_select {n_select} out of 1..{self.max_blocks}")
+        shape = (q.shape[0], self.n_kv_heads, n_select)
+        nbytes = self.workspace_bytes(q.shape[0], q.shape[1], n_select)
+        with self._on(stream):
+            if out is None:
+                out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            else:
+                self._is("out", out, torch.int32, shape)
+                if not out.is_contiguous():
+                    raise ValueError("out must be contiguous")
+            cerberus_page_select(pages, self.table, q, out, torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        return out
+
+    def attention(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, blocks: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """softmax(scale q K^T) V of one token q [batch][n_heads][head_dim] per sequence; scale: 1 / sqrt(head_dim)."""
+        self._query("q", q)
+        pages = self._layer(layer)
+        n_select = 0
+        if blocks is not None:
+            self._is("blocks", blocks, torch.int32, (q.shape[0], self.n_kv_heads, None))
+            n_select = blocks.shape[2]
+            if n_select < 1 or not blocks.is_contiguous():
+                raise ValueError("blocks must be contiguous and name at least one block")
+        nbytes = self.workspace_bytes(q.shape[0], q.shape[1], n_select)
+        with self._on(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            else:
+                self._query("out", out)
+                if out.shape != q.shape:
+                    raise ValueError("out has another shape than q")
+            cerberus_paged_attention(pages, self.table, q, out, self.head_dim ** -0.5 if scale is None else scale, blocks,
+                                     torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        return out
+
+
 class Engine:
     """A context plus the buffers that must outlive it, but for W["embed"] (fp32 mode: and W["lm_head"]): keep W for as long as
     the engine runs.  An engine whose dict is gone reads whatever the allocator puts there next."""
@@ -302,6 +512,54 @@ class Engine:
     def decode(self, st: DeviceState, batch: int, n_steps: int, out_tokens: torch.Tensor, out_count: torch.Tensor,
                stream=None):
         cerberus_decode(self.ctx, st.struct, batch, n_steps, out_tokens, out_count, stream)
+
+    def paged_step(self, st: DeviceState, cache: PageCache, batch: int, new_rows: Optional[torch.Tensor] = None, n_select: int = 0,
+                   stream=None):
+        """ar_step with the cache in pages: new_rows[b] 1 decodes a token, 0 sits out, below 0 ends the sequence."""
+        if cache.n_layers != self.cfg["n_layers"]:
+            raise ValueError("a page cache of another number of layers than the model")
+        if new_rows is not None:
+            cache._is("new_rows", new_rows, torch.int32, (batch,))
+            if not new_rows.is_contiguous():
+                raise ValueError("new_rows must be contiguous")
+        nbytes = cache.workspace_bytes(batch, self.cfg["n_heads"], n_select)
+        with cache._on(stream):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+            cerberus_paged_step(self.ctx, st.struct, cache.layers, cache.table, batch, new_rows, n_select, ws)
+
+    def move_prompts(self, st: DeviceState, cache: PageCache, lens: Sequence[int], stream=None) -> PagePlan:
+        """Rows 0..lens[b]-1 of the slab's sequences (0: none) become the next rows of the page cache's: what a prompt phase
+        leaves goes on in pages, and the slab's places are free for other prompts."""
+        if cache.n_layers != self.cfg["n_layers"] or not 1 <= len(lens) <= min(cache.max_seqs, self.max_batch) or \
+                min(lens) < 0 or max(lens) > self.kv_capacity:
+            raise ValueError("lens do not fit the slab or the page cache")
+        with cache._on(stream):
+            plan = cache.plan(torch.tensor(lens, dtype=torch.int32, device=cache.device), sum(lens))
+            at = 0
+            for b, n in enumerate(lens):
+                for l in range(cache.n_layers if n else 0):
+                    kv = st.kv[l, :, b, :, :n]                     # [2][heads][n][head_dim]
+                    cache.store(l, kv[0].transpose(0, 1), kv[1].transpose(0, 1), plan.slot[at:at + n])
+                at += n
+        return plan
+
+    def generate_paged(self, st: DeviceState, cache: PageCache, prompts, n_steps: int, n_select: int = 0, stream=None):
+        """Prompt phase in the slab, then n_steps one-token steps in pages; returns the committed token ids of every sequence
+        (fewer where the pages ran out) and ends the sequences."""
+        batch = len(prompts)
+        with cache._on(stream):
+            st.kv_len[:batch] = 0
+            for b, p in enumerate(prompts):
+                self.prefill(st, batch, b, p.to(device="cuda", dtype=torch.int32))
+            self.move_prompts(st, cache, [len(p) for p in prompts])
+            log = torch.full((batch, n_steps), -1, dtype=torch.int32, device="cuda")
+            here = (cache.kv_len[:batch] > 0).to(torch.int32)      # a prompt that found no pages decodes nothing
+            for i in range(n_steps):
+                self.paged_step(st, cache, batch, here, n_select)
+                log[:, i] = torch.where(st.accept_len[:batch] > 0, st.accepted_tokens[:batch, 0], -1)
+            cache.plan(torch.full((batch,), -1, dtype=torch.int32, device="cuda"), 0)
+            out = log.cpu()
+        return [[t for t in row if t >= 0] for row in out.tolist()]
 
     def generate(self, st: DeviceState, prompts, n_steps: int, stream=None):
         """Prompt phase for every sequence, then n_steps chained decoding steps (Algorithm 1 from its

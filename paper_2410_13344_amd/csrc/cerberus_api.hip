@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "paged.h"
 #include "step_kernels.h"
 
 using namespace cerb;
@@ -24,6 +25,18 @@ int fail(int code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
+
+}  // namespace
+
+int cerb::set_error(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+namespace {
 
 #define HIP_TRY(expr)                                                                              \
   do {                                                                                             \
@@ -693,10 +706,45 @@ int attn_per_head(const cerberus_ctx* c, const AttnShape& sh) {
   return att_items(c->D, sh.batch, sh.T, c->attn_chunk, per_head) <= room ? per_head : room - sh.batch * (1 + ceil_div(sh.T, 64));
 }
 
+// A step over pages: the layers' pages, the tables, and its scratch
+struct PagedStep {
+  const cerberus_pages* layers;
+  const cerberus_page_table* pt;
+  PagedWorkspace ws;
+  int n_select;
+};
+
+// Layer l's new rows (row b: sequence b) go to their slots, then each attends to its sequence's pages
+int run_paged_attention(const cerberus_ctx* c, const PagedStep& pp, int l, int batch, hipStream_t s) {
+  const Dims& D = c->D;
+  const bool bf16 = D.dtype == CERBERUS_BF16;
+  const size_t lo = (size_t)c->R64 * D.d;
+  const int shift = page_shift_of(pp.pt->page_size);
+  const void *k = bf16 ? c->ktree : pp.ws.k_rows, *v = bf16 ? c->vtree : pp.ws.v_rows;
+  const cerberus_pages& pg = pp.layers[l];
+  HIP_TRY(launch_page_store(PageStoreArgs{pg, k, v, D.d, D.dh, D.d, D.dh, pp.ws.slot, batch, shift, pp.pt->status}, s));
+  if (pp.n_select) {
+    PageSelectArgs a{};
+    a.pg = pg; a.table = pp.pt->block_table; a.lens = pp.ws.lens; a.max_blocks = pp.pt->max_blocks; a.page_shift = shift;
+    a.q = c->q; a.q_lo_off = bf16 ? lo : 0; a.q_row = D.d; a.batch = batch; a.n_heads = D.nH; a.n_select = pp.n_select;
+    a.blocks = pp.ws.blocks; a.keys = pp.ws.keys;
+    HIP_TRY(launch_page_select(a, s));
+  }
+  PagedAttnArgs a{};
+  a.pg = pg; a.table = pp.pt->block_table; a.lens = pp.ws.lens; a.max_blocks = pp.pt->max_blocks; a.page_shift = shift;
+  a.q = c->q; a.q_lo_off = bf16 ? lo : 0; a.q_row = D.d; a.out = c->attn; a.out_lo_off = bf16 ? lo : 0; a.out_row = D.d;
+  a.batch = batch; a.n_heads = D.nH; a.scale = 1.f / std::sqrt((float)D.dh); a.blocks = pp.n_select ? pp.ws.blocks : nullptr;
+  a.n_select = pp.n_select; a.part = pp.ws.part; a.status = pp.pt->status;
+  if (bf16) { a.own_k_lo = (const bf16_t*)c->ktree + lo; a.own_v_lo = (const bf16_t*)c->vtree + lo; a.own_row = D.d; }
+  HIP_TRY(launch_paged_attention(a, D.dtype, s));
+  return CERBERUS_OK;
+}
+
 // Embedding and the decoder layers over the rows the assembly kernel laid out; `tr` supplies the attention mask
-// (candidate tree, or a chain).  *pending: the GEMM whose partials are still to be added to x.
+// (candidate tree, or a chain).  *pending: the GEMM whose partials are still to be added to x.  pages: the cache is not st's
+// slab but these.
 int forward_rows(cerberus_ctx* c, const cerberus_state* st, int rows_max, const TreeDev& tr, const AttnShape& sh, GemmProb* pending,
-                 hipStream_t s) {
+                 hipStream_t s, const PagedStep* pages = nullptr) {
   const Dims& D = c->D;
   const RowMap& rm = c->rm;
   const size_t kv_layer_bytes = (size_t)2 * D.Bmax * D.nH * D.cap * D.dh * c->elem;
@@ -714,25 +762,30 @@ int forward_rows(cerberus_ctx* c, const cerberus_state* st, int rows_max, const 
     HIP_TRY(launch_add_gain(D, rm, c->x, prev ? prev->out : nullptr, prev ? prev->S : 0, prev ? prev->S_dev : nullptr,
                             prev ? (size_t)prev->out_rows * prev->N : 0, c->attn_norm[l], c->xn, c->ssq, rows_max, s, fq ? A_FRAG64 : tq ? A_FRAG : A_ROWS));
     GemmProb pq, po, pg;
-    void* kv_layer = (unsigned char*)st->kv + (size_t)l * kv_layer_bytes;
+    void* kv_layer = pages ? nullptr : (unsigned char*)st->kv + (size_t)l * kv_layer_bytes;
     if (fq) {
       TRY(run_fused_qkv(c, l, kv_layer, s));
     } else if (tq) {
       TRY(run_tile_qkv(c, l, kv_layer, rm.n_rows, rows_max, s));
     } else {
       TRY(run_gemm(c, c->p_qkv[l], rm.n_rows, 0, rows_max, nullptr, 0, s, &pq, qkv_split));
-      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, kv_layer, c->ktree, c->vtree,
-                             c->ssq, rows_max, s));
+      const bool rows = pages && D.dtype == CERBERUS_F32;   // (bf16 mode has planes of the new rows anyway)
+      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, kv_layer, rows ? pages->ws.k_rows : c->ktree,
+                             rows ? pages->ws.v_rows : c->vtree, c->ssq, rows_max, s));
     }
-    AttnArgs aa{};
-    aa.q = c->q; aa.q_lo_off = D.dtype == CERBERUS_BF16 ? (size_t)c->R64 * D.d : 0; aa.kv = kv_layer; aa.ktree = c->ktree; aa.vtree = c->vtree; aa.out = c->attn; aa.out_lo_off = (size_t)c->R64 * D.d; aa.part_o = c->attn_po; aa.part_ml = c->attn_ml; aa.rm = rm;
-    aa.anc = tr.anc; aa.aw = tr.aw; aa.Tpad = (int)align_up((size_t)sh.T, 64); aa.tc_max = ceil_div(sh.T, 64); aa.piece = sh.piece; aa.seq0 = sh.seq0;
-    aa.batch = sh.batch; aa.Bmax = D.Bmax; aa.nH = D.nH; aa.dh = D.dh; aa.cap = D.cap;
-    aa.chunk = c->attn_chunk; aa.part_rows = c->att_rows;
-    aa.att_cap = c->att_cap;
-    aa.grid_x = att_items(D, sh.batch, sh.T, c->attn_chunk, attn_per_head(c, sh));   // every item gets a workgroup per head
-    aa.rows_max = rows_max; aa.status = st->status;
-    HIP_TRY(launch_attention(aa, D.dtype, c->use_mfma_attn, s));
+    if (pages) {
+      TRY(run_paged_attention(c, *pages, l, sh.batch, s));
+    } else {
+      AttnArgs aa{};
+      aa.q = c->q; aa.q_lo_off = D.dtype == CERBERUS_BF16 ? (size_t)c->R64 * D.d : 0; aa.kv = kv_layer; aa.ktree = c->ktree; aa.vtree = c->vtree; aa.out = c->attn; aa.out_lo_off = (size_t)c->R64 * D.d; aa.part_o = c->attn_po; aa.part_ml = c->attn_ml; aa.rm = rm;
+      aa.anc = tr.anc; aa.aw = tr.aw; aa.Tpad = (int)align_up((size_t)sh.T, 64); aa.tc_max = ceil_div(sh.T, 64); aa.piece = sh.piece; aa.seq0 = sh.seq0;
+      aa.batch = sh.batch; aa.Bmax = D.Bmax; aa.nH = D.nH; aa.dh = D.dh; aa.cap = D.cap;
+      aa.chunk = c->attn_chunk; aa.part_rows = c->att_rows;
+      aa.att_cap = c->att_cap;
+      aa.grid_x = att_items(D, sh.batch, sh.T, c->attn_chunk, attn_per_head(c, sh));   // every item gets a workgroup per head
+      aa.rows_max = rows_max; aa.status = st->status;
+      HIP_TRY(launch_attention(aa, D.dtype, c->use_mfma_attn, s));
+    }
     if (tq) TRY(run_tile_planes(c, c->p_o[l], D.d, rm.n_rows, rows_max, &po, s));
     else TRY(run_gemm(c, c->p_o[l], rm.n_rows, 0, rows_max, nullptr, 0, s, &po));
     HIP_TRY(launch_add_gain(D, rm, c->x, po.out, po.S, po.S_dev, (size_t)po.out_rows * po.N, c->ffn_norm[l], c->xn, c->ssq, rows_max, s,
@@ -818,6 +871,23 @@ int run_step(cerberus_ctx* c, const cerberus_state* st, int batch, void* stream,
   HIP_TRY(launch_gate(D.d, D.threshold, c->h_last, c->last_row, c->taps.forced_gate_hidden, rm.seq_T, batch, st->entropy,
                       st->gate_flag, heads_prep(c), D.dtype, s));
   return run_heads(c, st, batch, s);
+}
+
+// The one-token step with the cache in pages
+int run_paged_step(cerberus_ctx* c, const cerberus_state* st, const PagedStep& pp, int batch, const int* new_rows, hipStream_t s) {
+  const Dims& D = c->D;
+  cerberus_state in_pages = *st;
+  in_pages.kv = nullptr;
+  in_pages.kv_len = pp.pt->kv_len;          // (the acceptance writes the length that the plan has put there already)
+  HIP_TRY(launch_page_plan(*pp.pt, new_rows, 1, batch, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, s));
+  HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
+  GemmProb pd{};
+  TRY(forward_rows(c, &in_pages, batch, c->tree, AttnShape{1, batch, 0, 0}, &pd, s, &pp));
+  TRY(run_lm_head(c, pd, nullptr, batch, s));
+  HIP_TRY(launch_accept(D, c->tree, c->rm, c->g, c->rm.row_tok, in_pages, c->path, c->last_row, batch, s));
+  HIP_TRY(launch_gate(D.d, D.threshold, c->h_last, c->last_row, c->taps.forced_gate_hidden, c->rm.seq_T, batch, st->entropy,
+                      st->gate_flag, heads_prep(c), D.dtype, s));
+  return run_heads(c, &in_pages, batch, s);
 }
 
 // Prompt phase for one sequence: passes of whole pieces, each a chain (causal mask, positions
@@ -1012,6 +1082,31 @@ int cerberus_verify_step(cerberus_ctx* ctx, const cerberus_state* st, int32_t ba
 
 int cerberus_ar_step(cerberus_ctx* ctx, const cerberus_state* st, int32_t batch, void* stream) {
   return run_step(ctx, st, batch, stream, ASSEMBLE_FORCE_AR);
+}
+
+int cerberus_paged_step(cerberus_ctx* ctx, const cerberus_state* st, const cerberus_pages* layers, const cerberus_page_table* pt,
+                        int32_t batch, const int32_t* new_rows, int32_t n_select, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+  if (!ctx || !st || !layers) return fail(CERBERUS_ERR_ARG, "null context, state or pages");
+  cerberus_state with = *st;                 // (a step over pages does without the slab and its lengths)
+  with.kv = with.kv_len = pt ? pt->kv_len : nullptr;
+  TRY(check_page_table(pt, batch));
+  TRY(check_state(ctx, &with, batch));
+  const Dims& D = ctx->D;
+  if (n_select < 0) return fail(CERBERUS_ERR_ARG, "n_select < 0");
+  for (int l = 0; l < D.n_layers; ++l) {
+    TRY(check_pages(layers + l));
+    TRY(check_same_pages(layers + l, pt));
+    if (layers[l].dtype != D.dtype || layers[l].n_kv_heads != D.nH || layers[l].head_dim != D.dh)
+      return fail(CERBERUS_ERR_SHAPE, "pages of layer %d differ from the model in dtype, heads or head_dim", l);
+    if (n_select && !layers[l].bounds) return fail(CERBERUS_ERR_ARG, "n_select needs the bounds of layer %d's pages", l);
+  }
+  const size_t need = cerberus_paged_workspace_bytes(layers, pt, batch, D.nH, n_select);
+  if (need == 0) return CERBERUS_ERR_ARG;    // (its text stands)
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256) return fail(CERBERUS_ERR_ARG, "workspace must be 256-byte aligned");
+  if (workspace_bytes < need) return fail(CERBERUS_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const PagedStep pp{layers, pt, paged_workspace(*layers, *pt, batch, D.nH, n_select, workspace), n_select};
+  return run_paged_step(ctx, st, pp, batch, new_rows, reinterpret_cast<hipStream_t>(stream));
 }
 
 int cerberus_prefill(cerberus_ctx* ctx, const cerberus_state* st, int32_t batch, int32_t seq, const int32_t* tokens,

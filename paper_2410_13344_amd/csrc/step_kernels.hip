@@ -212,6 +212,43 @@ hipError_t launch_assemble(const Dims& D, const TreeDev& tr, const RowMap& rm, c
   return hipGetLastError();
 }
 
+// Rows of a step over pages: row b is sequence b, one token, in every launch of the batch; a sequence that sits the step
+// out has a row nobody looks at (token 0, no slot, nothing to attend to, outside the taps).  slot: of the packed rows in, of the
+// sequences out.
+__global__ __launch_bounds__(64) void k_assemble_pages(const Dims D, const RowMap rm, const cerberus_state st, const cerberus_taps tp,
+                                                       int batch, const int* row_start, const int* first_pos, int* slot, int* lens) {
+  const int b = threadIdx.x;
+  bool runs = false;
+  int own = -1;
+  if (b < batch) {
+    runs = first_pos[b] >= 0 && row_start[b + 1] > row_start[b];
+    if (runs) own = slot[row_start[b]];
+  }
+  __syncthreads();                          // every packed slot has been read
+  if (b == 0) *rm.n_rows = batch;
+  if (b >= batch) return;
+  const int L = runs ? first_pos[b] : 0;
+  int tok = runs ? st.root_token[b] : 0;
+  if (tok < 0 || tok >= D.V) { atomicOr(st.status, (int)CERBERUS_DEV_BAD_TOKEN); tok = 0; }
+  slot[b] = own;
+  lens[b] = runs ? L + 1 : 0;
+  rm.seq_row0[b] = b;
+  rm.seq_T[b] = runs;
+  rm.seq_L[b] = L;
+  rm.row_seq[b] = b;
+  rm.row_node[b] = runs ? 0 : D.T;
+  rm.row_pos[b] = L;
+  rm.row_tok[b] = tok;
+  if (tp.node_token && runs) tp.node_token[b * D.T] = tok;
+}
+
+hipError_t launch_assemble_pages(const Dims& D, const RowMap& rm, const cerberus_state& st, const cerberus_taps& tp, int batch,
+                                 const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s) {
+  static_assert(CERBERUS_MAX_BATCH <= 64, "a thread per sequence, one wave");
+  hipLaunchKernelGGL(k_assemble_pages, dim3(1), dim3(64), 0, s, D, rm, st, tp, batch, row_start, first_pos, slot, lens);
+  return hipGetLastError();
+}
+
 // End of a prompt pass's layers: the rows are where they belong already (row L + i), so committing them is advancing
 // kv_len.  In the last pass the row map then becomes that of the tail (the rows of the prompt's last piece, which alone
 // go through the final norm and the LM head): rows 0.. of the head's buffers are the pass's rows tail[0]... ; the last of
@@ -527,12 +564,14 @@ __global__ void k_rope_kv(const float* __restrict__ part, int S, size_t pstride,
   st_a(q + (size_t)r * d + c1, q_lo_off, v[0] * sn + v[1] * cs);
   const float k0 = v[2] * cs - v[3] * sn, k1 = v[2] * sn + v[3] * cs;
   const size_t row = (size_t)(rm.seq_L[b] + node);
-  T* Kr = kv_layer + (((size_t)(0 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
-  T* Vr = kv_layer + (((size_t)(1 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
-  st_f(Kr + j, k0);
-  st_f(Kr + j + half, k1);
-  st_f(Vr + j, v[4]);
-  st_f(Vr + j + half, v[5]);
+  if (kv_layer) {   // (a step over pages stores the rows itself)
+    T* Kr = kv_layer + (((size_t)(0 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
+    T* Vr = kv_layer + (((size_t)(1 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
+    st_f(Kr + j, k0);
+    st_f(Kr + j + half, k1);
+    st_f(Vr + j, v[4]);
+    st_f(Vr + j + half, v[5]);
+  }
   if (ktree) {
     // This step's attention reads the tree rows from these hi+lo planes instead: rounding a new
     // row to one bf16 before its own step uses it is the largest single error of the bf16 path
@@ -551,7 +590,7 @@ hipError_t launch_rope_kv(const Dims& D, const RowMap& rm, const float* part, in
   dim3 grid(rows_max, D.nH), block(D.dh / 2);
   if (D.dtype == 0)
     hipLaunchKernelGGL((k_rope_kv<float>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (float*)q, (size_t)0,
-                       (float*)kv_layer, (float*)nullptr, (float*)nullptr, ssq, nb, D);
+                       (float*)kv_layer, (float*)ktree, (float*)vtree, ssq, nb, D);
   else
     hipLaunchKernelGGL((k_rope_kv<bf16_t>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (bf16_t*)q,
                        (size_t)D.R64 * D.d, (bf16_t*)kv_layer, (bf16_t*)ktree, (bf16_t*)vtree, ssq, nb, D);
