@@ -1,97 +1,484 @@
-// Attention of one new token per sequence over a key-value cache in pages.
+// Attention of one new token per sequence over a key-value cache in pages: out = softmax(scale q K^T) V.
 #include "paged.h"
+
+#include <limits.h>
+
+#include <algorithm>
 
 namespace cerb {
 
-// A workgroup per (sequence, head): DH / 4 lanes hold one key's row, four elements each, every key slot with a running
-// softmax of its own, merged at the end.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_paged_attn(const PagedAttnArgs a) {
-  constexpr int LPK = DH / 4, SLOTS = 256 / LPK;
-  const int b = blockIdx.x, h = blockIdx.y, hk = h / (a.n_heads / a.pg.n_kv_heads);
-  const int slot = threadIdx.x / LPK, e0 = (threadIdx.x % LPK) * 4;
-  const int ps = a.pg.page_size, L = min(max(a.lens[b], 0), a.max_blocks * ps), held = (L + ps - 1) / ps;
-  const T* q = reinterpret_cast<const T*>(a.q) + b * a.q_row + h * DH + e0;
-  float qv[4], o[4];
+namespace {
+
+// How the rows of a batch are cut.  Sequence b has rows_of(b) rows to look at (with chosen blocks: the rows of all places of
+// its list); they are cut into pieces of `piece` rows, a multiple of what a workgroup takes at a time, and every (piece, key
+// head, 16 of its query heads) is a workgroup.  A sequence of one piece is written out by its workgroup, the pieces of
+// others are joined by k_paged_join.  Every wave finds its place in that list by itself, from the lengths on the device.
+struct Cut {
+  int piece;        // rows
+  int b;            // sequence of the asked item, -1: behind the end
+  int j, pieces;    // which of its pieces, how many
+  int slot0;        // partial results of the cut sequences before it
+};
+
+__device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int b) {
+  const int L = min(max(a.lens[b], 0), a.max_blocks << a.page_shift);
+  return a.blocks && L > 0 ? a.n_select << a.page_shift : L;
+}
+
+// item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks after sequences l * k .. l * k + k - 1.
+__device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
+  const int lane = threadIdx.x & 63, k = (a.batch + 63) >> 6, b0 = lane * k, b1 = min(a.batch, b0 + k);
+  long long total = 0;
+  for (int b = b0; b < b1; ++b) total += rows_of(a, b);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    qv[e] = ld_f(q + e);
-    if (a.q_lo_off) qv[e] += ld_f(q + a.q_lo_off + e);
-    qv[e] *= a.scale;
-    o[e] = 0.f;
+  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+  Cut c;
+  // as many pieces as the launch has workgroups for: at most per_head + one per sequence
+  const long long want = (total + per_head - 1) / per_head;
+  c.piece = (int)min((max(want, 1ll) + unit - 1) / unit * unit, (long long)INT_MAX);   // (at INT_MAX nothing is cut)
+  auto pieces_of = [&](int b) { return max(1, (int)(((unsigned)rows_of(a, b) + (unsigned)c.piece - 1u) / (unsigned)c.piece)); };
+  int n = 0, cuts = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int p = pieces_of(b);
+    n += p;
+    cuts += p > 1 ? p : 0;
   }
-  float m = -INFINITY, l = 0.f;
-  const int nk = a.blocks ? a.n_select * ps : L;
-  for (int p0 = 0; p0 < nk; p0 += SLOTS) {
-    const int p = p0 + slot;
-    int blk = min(p, nk - 1) / ps;
-    const int off = p & (ps - 1);
-    bool vis = p < nk;
-    if (a.blocks) blk = a.blocks[((size_t)b * a.pg.n_kv_heads + hk) * a.n_select + blk];
-    vis = vis && blk >= 0 && blk < held && (long long)blk * ps + off < L;
-    const int page = vis ? a.table[(size_t)b * a.max_blocks + blk] : 0;
-    if (page < 0 || page >= a.pg.n_pages) { vis = false; atomicOr(a.status, (int)CERBERUS_DEV_BAD_PAGE); }
-    float kv[4] = {0.f, 0.f, 0.f, 0.f}, vv[4] = {0.f, 0.f, 0.f, 0.f};
-    if (vis) {
-      const size_t row = ((size_t)page * a.pg.n_kv_heads + hk) * ps + off;
+  int n_end = n, cut_end = cuts;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        kv[e] = ld_f(reinterpret_cast<const T*>(a.pg.k) + row * DH + e0 + e);
-        vv[e] = ld_f(reinterpret_cast<const T*>(a.pg.v) + row * DH + e0 + e);
-      }
-      if (a.own_k_lo && blk * ps + off == L - 1) {
+  for (int off = 1; off < 64; off <<= 1) {
+    const int x = __shfl_up(n_end, off, 64), y = __shfl_up(cut_end, off, 64);
+    if (lane >= off) { n_end += x; cut_end += y; }
+  }
+  const unsigned long long mine = __ballot(of_seq ? item >= b0 && item < b1 : item >= n_end - n && item < n_end);
+  c.b = -1;
+  c.j = c.pieces = c.slot0 = 0;
+  if (mine == 0) return c;
+  const int owner = __ffsll((long long)mine) - 1;
+  int at = __shfl(n_end - n, owner, 64), slot = __shfl(cut_end - cuts, owner, 64);
+  for (int b = owner * k; b < a.batch; ++b) {
+    const int p = pieces_of(b);
+    if (of_seq ? b == item : item < at + p) {
+      c.b = b; c.j = of_seq ? 0 : item - at; c.pieces = p; c.slot0 = slot;
+      break;
+    }
+    at += p;
+    slot += p > 1 ? p : 0;
+  }
+  return c;
+}
+
+template <typename T> struct Tile;      // 16-key tiles a wave takes at a time
+template <> struct Tile<bf16_t> { static constexpr int U = 2; };
+template <> struct Tile<float> { static constexpr int U = 1; };
+template <typename T> constexpr int kUnit = 4 * 16 * Tile<T>::U;   // rows that the four waves of a workgroup take at a time
+
+// What a wave holds of its tiles: K in the order of the first product's fragments, V rows as they lie.
+template <typename T, int DH> struct Stage;
+template <int DH> struct Stage<bf16_t, DH> {
+  uint4 k[2][DH / 32];                  // [tile][k-step]: key lane % 16, columns ks * 32 + (lane / 16) * 8 ..
+  uint32_t v[8][DH / 32];               // [tile * 4 + i]: key 4 * (lane / 16) + i, columns (lane % 16) * DH / 16 ..
+  int rows[2];                          // rows of every tile that count
+  int place;                            // own row's place in the wave's tiles, -1: not here (a step over pages)
+};
+template <int DH> struct Stage<float, DH> {
+  float4 k[1][DH / 16];                 // key lane % 16, columns s * 16 + (lane / 16) * 4 ..
+  float4 v[4][DH / 64];                 // key 4 * (lane / 16) + i, columns r * 64 + (lane % 16) * 4 ..
+  int rows[1];
+  int place;
+};
+
+}  // namespace
+
+// ---------------------------------------------------------------------------------------------
+// A workgroup takes a piece of one sequence's rows for one key head and up to 16 of the query heads that share it; its four
+// waves take tiles of the piece in turn, each with a running softmax of its own, joined at the end.  The work is bound by
+// the bytes of K and V, each used once, so everything goes from memory straight into registers in the order that the
+// matrix instructions want; there is no barrier in the loop, and a wave has the next tiles' loads in flight while it works.
+//   S^T = K Q^T   A = 16 keys, B = up to 16 queries (the columns of missing ones are thrown away: with one query per key
+//                 head the instructions are 15/16 idle and still not what takes the time)
+//                 -> lane: query lane % 16, keys 4 * (lane / 16) + i
+//   O^T = V^T P^T B = P^T straight from the S^T registers.  bf16: contraction slot 8 g + 4 u + i of the 32-key product is
+//                 key 4 g + i of tile u, so a lane's own scores are its fragment; A = V^T: lane (n, g) has loaded whole pieces
+//                 of the eight V rows of those slots, columns n * DH / 16 + j, and the fragment of product j is column j of that
+//                 8 x DH/16 square, turned around within the lane by byte permutes.  Product j gives columns j, j + DH / 16, ..
+//                 fp32: product (r, c, i) contracts keys 4 g + i over g and gives columns 64 r + 4 n + c.
+// A lane's outputs all belong to its query, so the running maximum's factor is the lane's own.
+// bf16: probabilities go into the second product as two bf16 planes (p to 2^-17): the matrix units have time.
+// STEP: a decoding step's queries and outputs are two bf16 planes, and the newest row has a second plane next to the cache.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int DH, bool STEP>
+__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, int per_head) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int U = Tile<T>::U, DV = DH / 16, KS = BF ? DH / 32 : DH / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15, g = lane >> 4;
+  const int nkv = a.pg.n_kv_heads, group = a.n_heads / nkv;
+  const int hk = blockIdx.x % nkv, h0 = blockIdx.x / nkv * 16;      // key head; first of its queries
+  const Cut cut = find_cut(a, blockIdx.y, false, kUnit<T>, per_head);
+  if (cut.b < 0) return;                                            // (uniform over the workgroup)
+  const int b = __builtin_amdgcn_readfirstlane(cut.b), ps = a.pg.page_size;
+  const int L = min(max(a.lens[b], 0), a.max_blocks << a.page_shift), held = (int)(((long long)L + ps - 1) >> a.page_shift);
+  const int begin = __builtin_amdgcn_readfirstlane(cut.j * cut.piece);
+  const int end = (int)min((long long)begin + cut.piece, (long long)rows_of(a, b)), first = wave * 16 * U;
+  const int n_it = end - begin > first ? (end - begin - first - 1) / kUnit<T> + 1 : 0;   // rounds of this wave
+
+  const int h = hk * group + min(h0 + lq, group - 1);
+  const T* qrow = reinterpret_cast<const T*>(a.q) + b * a.q_row + h * DH;
+  uint4 qf[KS], ql[STEP ? KS : 1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          kv[e] += ld_f(reinterpret_cast<const T*>(a.own_k_lo) + b * a.own_row + hk * DH + e0 + e);
-          vv[e] += ld_f(reinterpret_cast<const T*>(a.own_v_lo) + b * a.own_row + hk * DH + e0 + e);
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const uint4*>(qrow + (BF ? s * 32 + g * 8 : s * 16 + g * 4));
+    if constexpr (STEP) ql[s] = *reinterpret_cast<const uint4*>(qrow + a.q_lo_off + s * 32 + g * 8);
+  }
+
+  // Pages of the next 64 tiles, one lane each: tile e of the wave is tile e % U of its round e / U.
+  int my_page = -1, my_rows = 0, my_off = 0, my_place = -1;
+  auto look_up = [&](int it) {
+    const long long row = begin + (long long)(it + lane / U) * kUnit<T> + first + (lane % U) * 16;
+    my_page = -1;
+    my_rows = 0;
+    my_off = (int)row & (ps - 1);
+    my_place = -1;
+    if (row < end) {
+      int blk = (int)(row >> a.page_shift);
+      if (a.blocks) blk = a.blocks[((size_t)b * nkv + hk) * a.n_select + blk];
+      if (blk >= 0 && blk < held) {
+        const int page = a.table[(size_t)b * a.max_blocks + blk], pos = (blk << a.page_shift) + my_off;
+        if (page >= 0 && page < a.pg.n_pages) {
+          my_page = page;
+          my_rows = min(max(L - pos, 0), 16);
+          if (STEP && L - 1 >= pos && L - 1 < pos + 16) my_place = L - 1 - pos;
+        } else {
+          atomicOr(a.status, (int)CERBERUS_DEV_BAD_PAGE);
         }
       }
     }
-    float s = (qv[0] * kv[0] + qv[1] * kv[1]) + (qv[2] * kv[2] + qv[3] * kv[3]);
+  };
+  const T* pool_k = reinterpret_cast<const T*>(a.pg.k);
+  const T* pool_v = reinterpret_cast<const T*>(a.pg.v);
+  auto load = [&](Stage<T, DH>& st, int it) {
+    constexpr int kRounds = 64 / U;
+    if (it % kRounds == 0) look_up(it);
+    st.place = -1;
 #pragma unroll
-    for (int off2 = LPK / 2; off2 > 0; off2 >>= 1) s += __shfl_xor(s, off2, 64);
-    if (vis && s != -INFINITY) {
-      const float mn = fmaxf(m, s), corr = expf(m - mn), pw = expf(s - mn);
-      l = l * corr + pw;
+    for (int u = 0; u < U; ++u) {
+      const int e = it % kRounds * U + u;
+      const int page = max(__builtin_amdgcn_readlane(my_page, e), 0), rows = __builtin_amdgcn_readlane(my_rows, e);   // (no rows: page 0, unused)
+      const size_t row0 = ((size_t)page * nkv + hk) * ps + __builtin_amdgcn_readlane(my_off, e);
+      const int last = max(rows - 1, 0);                            // rows that do not count are re-reads of the last one
+      st.rows[u] = rows;
+      if constexpr (STEP) {
+        const int place = __builtin_amdgcn_readlane(my_place, e);
+        if (place >= 0) st.place = u * 16 + place;
+      }
+      const T* kr = pool_k + (row0 + min(lq, last)) * DH;
+      if constexpr (BF) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = o[e] * corr + pw * vv[e];
-      m = mn;
+        for (int s = 0; s < KS; ++s) st.k[u][s] = *reinterpret_cast<const uint4*>(kr + s * 32 + g * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const T* vr = pool_v + (row0 + min(4 * g + i, last)) * DH + lq * DV;
+          if constexpr (DV == 8) {
+            const uint4 w = *reinterpret_cast<const uint4*>(vr);
+            st.v[u * 4 + i][0] = w.x; st.v[u * 4 + i][1] = w.y; st.v[u * 4 + i][2] = w.z; st.v[u * 4 + i][3] = w.w;
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(vr);
+            st.v[u * 4 + i][0] = w.x; st.v[u * 4 + i][1] = w.y;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) st.k[u][s] = *reinterpret_cast<const float4*>(kr + s * 16 + g * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < DH / 64; ++r)
+            st.v[i][r] = *reinterpret_cast<const float4*>(pool_v + (row0 + min(4 * g + i, last)) * DH + r * 64 + lq * 4);
+      }
+    }
+  };
+
+  constexpr int NA = BF ? DV : DH / 16;
+  f32x4_t acc[NA];
+#pragma unroll
+  for (int j = 0; j < NA; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                                     // l: of the lane's own keys
+  const float scale2 = a.scale * 1.44269504088896340736f;           // scores in powers of two
+
+  // bf16: the second product over the wave's 32 keys, V in vv
+  auto values = [&](const uint32_t (&vv)[8][DH / 32 > 0 ? DH / 32 : 1], const uint4& ph, const uint4& pl) {
+#pragma unroll
+    for (int j = 0; j < DV; ++j) {
+      uint4 f;
+      const unsigned sel = j & 1 ? 0x07060302u : 0x05040100u;
+      f.x = __builtin_amdgcn_perm(vv[1][j / 2], vv[0][j / 2], sel);
+      f.y = __builtin_amdgcn_perm(vv[3][j / 2], vv[2][j / 2], sel);
+      f.z = __builtin_amdgcn_perm(vv[5][j / 2], vv[4][j / 2], sel);
+      f.w = __builtin_amdgcn_perm(vv[7][j / 2], vv[6][j / 2], sel);
+      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, ph), acc[j], 0, 0, 0);
+      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, pl), acc[j], 0, 0, 0);
+    }
+  };
+
+  auto work = [&](Stage<T, DH>& st) {
+    f32x4_t s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        if constexpr (BF) {
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, st.k[u][k]), __builtin_bit_cast(bf16x8_t, qf[k]), s[u], 0, 0, 0);
+          if constexpr (STEP)
+            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, st.k[u][k]), __builtin_bit_cast(bf16x8_t, ql[k]), s[u], 0, 0, 0);
+        } else {
+          const float4 x = st.k[u][k], y = __builtin_bit_cast(float4, qf[k]);
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, y.x, s[u], 0, 0, 0);
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, y.y, s[u], 0, 0, 0);
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, y.z, s[u], 0, 0, 0);
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, y.w, s[u], 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (STEP) {
+      if (st.place >= 0) {                                          // what the cache's rounding left of the newest key
+        const T* kl = reinterpret_cast<const T*>(a.own_k_lo) + b * a.own_row + hk * DH;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            uint4 f = make_uint4(0, 0, 0, 0);
+            if (st.place == u * 16 + lq) f = *reinterpret_cast<const uint4*>(kl + k * 32 + g * 8);
+            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, qf[k]), s[u], 0, 0, 0);
+          }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[u][i] *= scale2;
+      if (st.rows[u] < 16) {                                        // (uniform over the wave)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool off = 4 * g + i >= st.rows[u];
+          if (off) s[u][i] = -INFINITY;
+          if constexpr (BF) {
+#pragma unroll
+            for (int w = 0; w < DH / 32; ++w) st.v[u * 4 + i][w] = off ? 0u : st.v[u * 4 + i][w];
+          } else {
+#pragma unroll
+            for (int r = 0; r < DH / 64; ++r) if (off) st.v[i][r] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[u][i]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mn = fmaxf(m, mx), base = mn == -INFINITY ? 0.f : mn;
+    const float fac = __builtin_amdgcn_exp2f(m - base);             // first tiles: 2^-inf = 0
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - base);
+        sum += s[u][i];
+      }
+    if (__ballot(fac != 1.f)) {
+      l *= fac;
+#pragma unroll
+      for (int j = 0; j < NA; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] *= fac;
+    }
+    l += sum;
+    if constexpr (BF) {
+      union { bf16_t e[8]; uint4 w; } ph, pl;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ph.e[u * 4 + i] = f32_to_bf16(s[u][i]);
+          pl.e[u * 4 + i] = f32_to_bf16(s[u][i] - bf16_to_f32(ph.e[u * 4 + i]));
+        }
+      values(st.v, ph.w, pl.w);
+      if constexpr (STEP) {
+        if (st.place >= 0) {
+          const T* vl = reinterpret_cast<const T*>(a.own_v_lo) + b * a.own_row + hk * DH + lq * DV;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int w = 0; w < DH / 32; ++w)
+              st.v[e][w] = st.place == (e / 4) * 16 + 4 * g + e % 4 ? *reinterpret_cast<const uint32_t*>(vl + 2 * w) : 0u;
+          values(st.v, ph.w, pl.w);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < DH / 64; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 x = st.v[i][r];
+          acc[r * 4 + 0] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, s[0][i], acc[r * 4 + 0], 0, 0, 0);
+          acc[r * 4 + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, s[0][i], acc[r * 4 + 1], 0, 0, 0);
+          acc[r * 4 + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, s[0][i], acc[r * 4 + 2], 0, 0, 0);
+          acc[r * 4 + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, s[0][i], acc[r * 4 + 3], 0, 0, 0);
+        }
+    }
+  };
+
+  Stage<T, DH> s0, s1;
+  if (n_it > 0) load(s0, 0);
+  for (int it = 0; it < n_it; it += 2) {
+    if (it + 1 < n_it) load(s1, it + 1);
+    work(s0);
+    if (it + 1 < n_it) {
+      if (it + 2 < n_it) load(s0, it + 2);
+      work(s1);
     }
   }
-  __shared__ float sm[SLOTS], sl[SLOTS], so[SLOTS][DH];
+
+  // the four waves' sums: to the highest maximum, then added
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  __shared__ float sm[4][16], sl[4][16];
+  __shared__ __attribute__((aligned(16))) float so[4][16][DH + 4];
+  if (g == 0) { sm[wave][lq] = m; sl[wave][lq] = l; }
+  const bool live = h0 + lq < group;
+  if (live) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) so[slot][e0 + e] = o[e];
-  if (e0 == 0) { sm[slot] = m; sl[slot] = l; }
-  __syncthreads();
-  const int t = threadIdx.x;
-  if (t >= DH) return;
-  float M = -INFINITY, num = 0.f, den = 0.f;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-  for (int j = 0; j < SLOTS; ++j) M = fmaxf(M, sm[j]);
-#pragma unroll
-  for (int j = 0; j < SLOTS; ++j) {
-    if (sl[j] == 0.f) continue;
-    const float w = expf(sm[j] - M);
-    den += w * sl[j];
-    num += w * so[j][t];
+      for (int j = 0; j < NA; ++j) {
+        const int d = BF ? DV * (4 * g + i) + j : (j / 4) * 64 + 4 * (4 * g + i) + j % 4;
+        so[wave][lq][d] = acc[j][i];
+      }
   }
-  const float r = den == 0.f ? 0.f : num / den;
-  T* out = reinterpret_cast<T*>(a.out) + b * a.out_row + h * DH + t;
-  if (a.out_lo_off) st_a(out, a.out_lo_off, r);
-  else st_f(out, r);
+  __syncthreads();
+  const int n_live = min(16, group - h0);
+  for (int t = threadIdx.x; t < n_live * (DH / 4); t += 256) {
+    const int q = t / (DH / 4), d = t % (DH / 4) * 4;
+    float M = sm[0][q];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) M = fmaxf(M, sm[w][q]);
+    float den = 0.f, num[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = sm[w][q] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][q] - M);
+      const float4 o = *reinterpret_cast<const float4*>(&so[w][q][d]);
+      den += f * sl[w][q];
+      num[0] += f * o.x; num[1] += f * o.y; num[2] += f * o.z; num[3] += f * o.w;
+    }
+    const int head = hk * group + h0 + q;
+    if (cut.pieces > 1) {
+      const size_t at = (size_t)(cut.slot0 + cut.j) * a.n_heads + head;
+      *reinterpret_cast<float4*>(a.part + at * DH + d) = make_float4(num[0], num[1], num[2], num[3]);
+      if (d == 0) {
+        float* ml = a.part + (size_t)2 * per_head * a.n_heads * DH + at * 2;
+        ml[0] = M;
+        ml[1] = den;
+      }
+    } else {
+      const float inv = den == 0.f ? 0.f : 1.f / den;               // nothing to look at: zeros
+      const float o[4] = {num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+      T* out = reinterpret_cast<T*>(a.out) + b * a.out_row + head * DH + d;
+      if constexpr (STEP) {
+        st_a4(out, a.out_lo_off, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st_f(out + e, o[e]);
+      }
+    }
+  }
 }
 
-size_t paged_attention_bytes(int, int, int, int, int, int, int) { return 256; }
+// Joins the pieces of a sequence: a workgroup per (head, sequence), groups of DH / 4 lanes take pieces in turn.
+template <typename T, int DH, bool STEP>
+__global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int unit, int per_head) {
+  constexpr int LPP = DH / 4, GROUPS = 256 / LPP;
+  const int h = blockIdx.x, b = blockIdx.y;
+  const Cut cut = find_cut(a, b, true, unit, per_head);
+  if (cut.pieces <= 1) return;                                      // written out already
+  const int t = threadIdx.x / LPP, d = threadIdx.x % LPP * 4;
+  const float* ml = a.part + (size_t)2 * per_head * a.n_heads * DH;
+  float M = -INFINITY, den = 0.f, num[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j = t; j < cut.pieces; j += GROUPS) {
+    const size_t at = (size_t)(cut.slot0 + j) * a.n_heads + h;
+    const float2 x = *reinterpret_cast<const float2*>(ml + at * 2);
+    const float4 o = *reinterpret_cast<const float4*>(a.part + at * DH + d);
+    const float mn = fmaxf(M, x.x), base = mn == -INFINITY ? 0.f : mn;
+    const float f0 = __builtin_amdgcn_exp2f(M - base), f1 = __builtin_amdgcn_exp2f(x.x - base);
+    M = mn;
+    den = den * f0 + x.y * f1;
+    num[0] = num[0] * f0 + o.x * f1; num[1] = num[1] * f0 + o.y * f1; num[2] = num[2] * f0 + o.z * f1; num[3] = num[3] * f0 + o.w * f1;
+  }
+  __shared__ float sm[GROUPS], sd[GROUPS];
+  __shared__ __attribute__((aligned(16))) float so[GROUPS][DH];
+  *reinterpret_cast<float4*>(&so[t][d]) = make_float4(num[0], num[1], num[2], num[3]);
+  if (d == 0) { sm[t] = M; sd[t] = den; }
+  __syncthreads();
+  if (t != 0) return;
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, sm[i]);
+  den = num[0] = num[1] = num[2] = num[3] = 0.f;
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const float f = sm[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[i] - M);
+    const float4 o = *reinterpret_cast<const float4*>(&so[i][d]);
+    den += f * sd[i];
+    num[0] += f * o.x; num[1] += f * o.y; num[2] += f * o.z; num[3] += f * o.w;
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const float o[4] = {num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv};
+  T* out = reinterpret_cast<T*>(a.out) + b * a.out_row + h * DH + d;
+  if constexpr (STEP) {
+    st_a4(out, a.out_lo_off, o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) st_f(out + e, o[e]);
+  }
+}
+
+namespace {
+
+constexpr int kTarget = 1024;     // workgroups a launch aims for, four per compute unit
+
+int head_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
+// pieces that a launch aims for per (key head, 16 queries)
+int per_head_of(int n_heads, int n_kv_heads) { return std::max(1, kTarget / (n_kv_heads * head_tiles(n_heads, n_kv_heads))); }
+
+template <typename T, int DH, bool STEP>
+void launch(const PagedAttnArgs& a, hipStream_t s) {
+  const int tiles = head_tiles(a.n_heads, a.pg.n_kv_heads), per_head = per_head_of(a.n_heads, a.pg.n_kv_heads);
+  // no sequence can be cut if all the table or the list has room for is one workgroup's turn
+  const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift;
+  const bool cuts = most > kUnit<T>;
+  const int items = a.batch + (cuts ? per_head : 0);
+  hipLaunchKernelGGL((k_paged_attn<T, DH, STEP>), dim3(a.pg.n_kv_heads * tiles, items), dim3(256), 0, s, a, per_head);
+  if (cuts) hipLaunchKernelGGL((k_paged_join<T, DH, STEP>), dim3(a.n_heads, a.batch), dim3(256), 0, s, a, kUnit<T>, per_head);
+}
+
+}  // namespace
+
+// partial results: cut sequences have at most 2 per_head pieces (see find_cut: a cut one has more than `piece` rows)
+size_t paged_attention_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int max_blocks, int page_size, int n_select) {
+  return (size_t)2 * per_head_of(n_heads, n_kv_heads) * n_heads * (head_dim + 2) * sizeof(float);
+}
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, hipStream_t s) {
-  dim3 grid(a.batch, a.n_heads);
   const bool wide = a.pg.head_dim == 128;
   if (dtype == CERBERUS_F32) {
-    if (wide) hipLaunchKernelGGL((k_paged_attn<float, 128>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_paged_attn<float, 64>), grid, dim3(256), 0, s, a);
+    if (wide) launch<float, 128, false>(a, s);
+    else launch<float, 64, false>(a, s);
+  } else if (a.own_k_lo) {
+    if (wide) launch<bf16_t, 128, true>(a, s);
+    else launch<bf16_t, 64, true>(a, s);
   } else {
-    if (wide) hipLaunchKernelGGL((k_paged_attn<bf16_t, 128>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_paged_attn<bf16_t, 64>), grid, dim3(256), 0, s, a);
+    if (wide) launch<bf16_t, 128, false>(a, s);
+    else launch<bf16_t, 64, false>(a, s);
   }
   return hipGetLastError();
 }
