@@ -140,7 +140,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _stream_ptr(stream) -> int:
     if stream is None:
         stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    return stream if type(stream) is int else stream.cuda_stream
 
 
 def make_config(cfg: dict, dtype: int, max_batch: int, kv_capacity: int) -> Config:
@@ -333,10 +333,11 @@ class PagePlan:
 
     def __init__(self, batch: int, max_rows: int, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
-        self.max_rows = max_rows
+        self.batch, self.max_rows, self.device = batch, max_rows, torch.device(device)
         self.row_start = torch.zeros(batch + 1, **i32)
         self.first_pos = torch.zeros(batch, **i32)
         self.slot = torch.full((max(max_rows, 1),), -1, **i32)
+        self.pointers = self.row_start.data_ptr(), self.first_pos.data_ptr(), self.slot.data_ptr()
 
 
 class PageCache:
@@ -354,7 +355,10 @@ class PageCache:
         if min(n_pages, page_size, n_kv_heads, head_dim, max_seqs, max_blocks) < 1 or n_layers < 0:
             raise ValueError("non-positive size of a page cache")
         self.dtype = torch.float32 if dtype == CERBERUS_F32 else torch.bfloat16
-        self.device = torch.device(device, torch.cuda.current_device()) if torch.device(device).index is None else torch.device(device)
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        device, self._index = self.device, self.device.index
         self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_layers, n_pages, page_size, n_kv_heads, head_dim
         self.max_seqs, self.max_blocks = max_seqs, max_blocks
         shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
@@ -375,6 +379,8 @@ class PageCache:
             self.layers[i] = Pages(self.k[i].data_ptr(), self.v[i].data_ptr(), self.bounds[i].data_ptr() if bounds else None,
                                    n_pages, page_size, n_kv_heads, head_dim, dtype)
         self._bytes = {}
+        self._refs = [C.byref(self.layers[i]) for i in range(n_layers)]      # (what ctypes makes of a struct on every call)
+        self._table, self._status = C.byref(self.table), self.status.data_ptr()
 
     def new_plan(self, batch: int, max_rows: int) -> PagePlan:
         return PagePlan(batch, max_rows, self.device)
@@ -383,99 +389,120 @@ class PageCache:
         key = (batch, n_heads, n_select)
         n = self._bytes.get(key)
         if n is None:
-            n = cerberus_paged_workspace_bytes(self._layer(0), self.table, batch, n_heads, n_select)
+            n = cerberus_paged_workspace_bytes(self.layers[0], self.table, batch, n_heads, n_select)
             if n == 0:
                 raise CerberusError(-2)
             self._bytes[key] = n
         return n
 
+    # A call takes about as long on the host as the smallest kernels run, so the methods below check in few steps, and only a
+    # call on a stream of its own, or from another device, pays for torch's context of it.
+    def _elsewhere(self, stream) -> bool:
+        return stream is not None or torch.cuda.current_device() != self._index
+
     def _on(self, stream):
         """Makes the cache's device and the call's stream torch's current ones."""
         return torch.cuda.stream(torch.cuda.current_stream(self.device) if stream is None else stream)
 
-    def _is(self, what: str, t: torch.Tensor, dtype, shape) -> None:
-        if t.dtype != dtype or t.device != self.device or t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
-            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {shape} on {self.device}")
+    def _stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self._index)
+
+    def _refuse(self, what: str, t: torch.Tensor, expected) -> None:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}, expected {expected} on {self.device}")
+
+    def _ints(self, what: str, t: torch.Tensor, shape) -> None:
+        if t.dtype is not torch.int32 or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            self._refuse(what, t, f"contiguous int32 {tuple(shape)}")
+
+    def _layer(self, layer: int):
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer {layer} out of 0..{self.n_layers - 1}")
+        return self._refs[layer]
 
     def plan(self, new_rows: torch.Tensor, max_rows: Optional[int] = None, out: Optional[PagePlan] = None, stream=None) -> PagePlan:
         """Places for the next rows of sequences 0..len(new_rows)-1.  max_rows: room of the slot map (with `out`: that plan's)."""
-        self._is("new_rows", new_rows, torch.int32, (None,))
-        batch = new_rows.shape[0]
-        if not new_rows.is_contiguous():
-            raise ValueError("new_rows must be contiguous")
-        with self._on(stream):
-            if out is None:
-                if max_rows is None:
-                    raise ValueError("plan needs max_rows or out")
-                out = PagePlan(batch, max_rows, self.device)
-            elif out.first_pos.shape[0] != batch or out.first_pos.device != self.device or (max_rows is not None and max_rows != out.max_rows):
-                raise ValueError("out is a plan of another batch, device or max_rows")
-            cerberus_page_plan(self.table, new_rows, out.max_rows, out.row_start, out.first_pos, out.slot)
+        if self._elsewhere(stream):
+            with self._on(stream):
+                return self.plan(new_rows, max_rows, out)
+        batch = new_rows.numel()
+        self._ints("new_rows", new_rows, (batch,))
+        if out is None:
+            if max_rows is None:
+                raise ValueError("plan needs max_rows or out")
+            out = PagePlan(batch, max_rows, self.device)
+        elif out.batch != batch or out.device != self.device or (max_rows is not None and max_rows != out.max_rows):
+            raise ValueError("out is a plan of another batch, device or max_rows")
+        _check(lib().cerberus_page_plan(self._table, new_rows.data_ptr(), batch, out.max_rows, *out.pointers, self._stream()))
         return out
 
     def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, stream=None) -> None:
         """Rows k, v [rows][n_kv_heads][head_dim] (any strides of rows and heads) into their slots."""
-        self._is("slot", slot, torch.int32, (None,))
-        shape = (slot.shape[0], self.n_kv_heads, self.head_dim)
-        self._is("k", k, self.dtype, shape)
-        self._is("v", v, self.dtype, shape)
-        pages = self._layer(layer)
-        if shape[0] == 0:
-            return
-        if k.stride(2) != 1 or v.stride(2) != 1 or not slot.is_contiguous():
-            raise ValueError("a row of k and v, and slot, must be contiguous")
-        with self._on(stream):
-            cerberus_page_store(pages, k, v, slot, self.status)
+        if self._elsewhere(stream):
+            with self._on(stream):
+                return self.store(layer, k, v, slot)
+        n = slot.numel()
+        self._ints("slot", slot, (n,))
+        shape = (n, self.n_kv_heads, self.head_dim)
+        pages, ks, vs = self._layer(layer), k.stride(), v.stride()
+        for what, t, s in (("k", k, ks), ("v", v, vs)):
+            if t.dtype is not self.dtype or t.shape != shape or t.device != self.device or s[2] != 1:
+                self._refuse(what, t, f"{self.dtype} {shape}, contiguous rows")
+        if n:
+            _check(lib().cerberus_page_store(pages, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], slot.data_ptr(), n,
+                                             self._status, self._stream()))
 
-    def _layer(self, layer: int) -> Pages:
-        if not 0 <= layer < self.n_layers:
-            raise ValueError(f"layer {layer} out of 0..{self.n_layers - 1}")
-        return self.layers[layer]
-
-    def _query(self, what: str, q: torch.Tensor) -> None:
-        self._is(what, q, self.dtype, (None, None, self.head_dim))
-        if q.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != self.head_dim):
-            raise ValueError(f"the heads of a row of {what} must be contiguous")
+    def _query(self, what: str, q: torch.Tensor):
+        """batch, heads, row stride"""
+        if q.dtype is self.dtype and q.device == self.device and q.dim() == 3:
+            (batch, heads, dim), s = q.shape, q.stride()
+            if dim == self.head_dim and s[2] == 1 and (heads == 1 or s[1] == dim):
+                return batch, heads, s[0]
+        self._refuse(what, q, f"{self.dtype} [batch][heads][{self.head_dim}], the heads of a row contiguous")
 
     def select(self, layer: int, q: torch.Tensor, n_select: int, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The n_select blocks of every sequence and key head that q [batch][n_heads][head_dim] attends to."""
-        self._query("q", q)
-        pages = self._layer(layer)
+        if self._elsewhere(stream):
+            with self._on(stream):
+                return self.select(layer, q, n_select, out)
+        batch, heads, row = self._query("q", q)
+        pages, shape = self._layer(layer), (batch, self.n_kv_heads, n_select)
         if not 1 <= n_select <= self.max_blocks:
             raise ValueError(f"n_select {n_select} out of 1..{self.max_blocks}")
-        shape = (q.shape[0], self.n_kv_heads, n_select)
-        nbytes = self.workspace_bytes(q.shape[0], q.shape[1], n_select)
-        with self._on(stream):
-            if out is None:
-                out = torch.empty(shape, dtype=torch.int32, device=self.device)
-            else:
-                self._is("out", out, torch.int32, shape)
-                if not out.is_contiguous():
-                    raise ValueError("out must be contiguous")
-            cerberus_page_select(pages, self.table, q, out, torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        nbytes = self.workspace_bytes(batch, heads, n_select)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        else:
+            self._ints("out", out, shape)
+        _check(lib().cerberus_page_select(pages, self._table, q.data_ptr(), row, batch, heads, n_select, out.data_ptr(), ws.data_ptr(),
+                                          nbytes, self._stream()))
         return out
 
     def attention(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, blocks: Optional[torch.Tensor] = None,
                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """softmax(scale q K^T) V of one token q [batch][n_heads][head_dim] per sequence; scale: 1 / sqrt(head_dim)."""
-        self._query("q", q)
-        pages = self._layer(layer)
-        n_select = 0
+        if self._elsewhere(stream):
+            with self._on(stream):
+                return self.attention(layer, q, scale, blocks, out)
+        batch, heads, row = self._query("q", q)
+        pages, n_select, picked = self._layer(layer), 0, None
         if blocks is not None:
-            self._is("blocks", blocks, torch.int32, (q.shape[0], self.n_kv_heads, None))
-            n_select = blocks.shape[2]
-            if n_select < 1 or not blocks.is_contiguous():
-                raise ValueError("blocks must be contiguous and name at least one block")
-        nbytes = self.workspace_bytes(q.shape[0], q.shape[1], n_select)
-        with self._on(stream):
-            if out is None:
-                out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-            else:
-                self._query("out", out)
-                if out.shape != q.shape:
-                    raise ValueError("out has another shape than q")
-            cerberus_paged_attention(pages, self.table, q, out, self.head_dim ** -0.5 if scale is None else scale, blocks,
-                                     torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+            n_select, picked = blocks.shape[-1], blocks.data_ptr()
+            self._ints("blocks", blocks, (batch, self.n_kv_heads, n_select))
+            if n_select < 1:
+                raise ValueError("blocks must name at least one block")
+        nbytes = self.workspace_bytes(batch, heads, n_select)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if out is None:
+            out = torch.empty((batch, heads, self.head_dim), dtype=self.dtype, device=self.device)
+            out_row = heads * self.head_dim
+        else:
+            out_batch, out_heads, out_row = self._query("out", out)
+            if out_batch != batch or out_heads != heads or (batch > 1 and abs(out_row) < heads * self.head_dim):
+                raise ValueError("out has another shape than q, or rows that overlap")
+        _check(lib().cerberus_paged_attention(pages, self._table, q.data_ptr(), row, out.data_ptr(), out_row, batch, heads,
+                                              self.head_dim ** -0.5 if scale is None else scale, picked, n_select, ws.data_ptr(), nbytes,
+                                              self._stream()))
         return out
 
 
@@ -519,9 +546,7 @@ class Engine:
         if cache.n_layers != self.cfg["n_layers"]:
             raise ValueError("a page cache of another number of layers than the model")
         if new_rows is not None:
-            cache._is("new_rows", new_rows, torch.int32, (batch,))
-            if not new_rows.is_contiguous():
-                raise ValueError("new_rows must be contiguous")
+            cache._ints("new_rows", new_rows, (batch,))
         nbytes = cache.workspace_bytes(batch, self.cfg["n_heads"], n_select)
         with cache._on(stream):
             ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)

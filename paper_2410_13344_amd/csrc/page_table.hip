@@ -3,6 +3,8 @@
 
 #include <limits.h>
 
+#include <algorithm>
+
 namespace cerb {
 
 namespace {
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
   __shared__ float sh[2][4][DH];
   const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
-  const int ps = a.pg.page_size, r_end = min(a.n_rows, (int)(blockIdx.x + 1) * chunk);
+  const int ps = a.pg.page_size, r_end = (int)min((long long)a.n_rows, (blockIdx.x + 1ll) * chunk);
   const long long slots = (long long)a.pg.n_pages * ps;
   const T* k = reinterpret_cast<const T*>(a.k) + h * a.k_head + piece * N;
   const T* v = reinterpret_cast<const T*>(a.v) + h * a.v_head + piece * N;
@@ -266,8 +268,14 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
   }
 }
 
+constexpr int kStoreWorkgroups = 2048;
+
 hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
-  const int chunk = 1;
+  // Workgroups for the whole card before any takes several runs: a row each while there are few (a decoding step's rows are
+  // runs of one), up to about a page of rows for prompts, whose runs are pages; never more than 2^20 along the rows.
+  const long long work = (long long)a.n_rows * a.pg.n_kv_heads;
+  int chunk = (int)std::min<long long>(std::max<long long>(1, work / kStoreWorkgroups), a.pg.page_size);
+  chunk = std::max(chunk, (a.n_rows - 1) / (1 << 20) + 1);
   dim3 grid((a.n_rows + chunk - 1) / chunk, a.pg.n_kv_heads);
   const bool wide = a.pg.head_dim == 128;
   if (a.pg.dtype == CERBERUS_F32) {

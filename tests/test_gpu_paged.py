@@ -757,3 +757,26 @@ def test_generate_paged_equals_generate_without_the_tree():
         torch.cuda.synchronize()
         assert got == want and int(cache.n_free) == 16 and cache.kv_len.tolist() == [0, 0]
     pair.engine.close()
+
+
+def test_entry_points_by_their_names():
+    """The calls of the header, one by one, on tensors of the caller's own."""
+    page, kv, heads, dh, n = 16, 2, 4, 64, 37
+    i32 = dict(dtype=torch.int32, device="cuda")
+    free, n_free, status = torch.arange(6, **i32), torch.tensor([6], **i32), torch.zeros(1, **i32)
+    table, lens = torch.full((1, 4), -1, **i32), torch.zeros(1, **i32)
+    pt = B.PageTable(table.data_ptr(), lens.data_ptr(), free.data_ptr(), n_free.data_ptr(), status.data_ptr(), 1, 4, page, 6)
+    k, v = torch.zeros(6, kv, page, dh, device="cuda"), torch.zeros(6, kv, page, dh, device="cuda")
+    bounds = torch.zeros(6, kv, 2, dh, device="cuda")
+    pg = B.Pages(k.data_ptr(), v.data_ptr(), bounds.data_ptr(), 6, page, kv, dh, F32)
+    row_start, first, slot = torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros(n, **i32)
+    B.cerberus_page_plan(pt, torch.tensor([n], **i32), n, row_start, first, slot)
+    rows = torch.randn(n, 2, kv, dh, device="cuda")
+    B.cerberus_page_store(pg, rows[:, 0], rows[:, 1], slot, status)
+    q = torch.randn(1, heads, dh, device="cuda")
+    ws = torch.empty(B.cerberus_paged_workspace_bytes(pg, pt, 1, heads, 2), dtype=torch.uint8, device="cuda")
+    blocks, out = torch.zeros(1, kv, 2, **i32), torch.zeros(1, heads, dh, device="cuda")
+    B.cerberus_page_select(pg, pt, q, blocks, ws)
+    B.cerberus_paged_attention(pg, pt, q, out, 0.125, blocks, ws)
+    assert table.tolist() == [[5, 4, 3, -1]] and int(status) == 0 and blocks.tolist() == [[[0, 2], [0, 2]]]
+    check_attention(out, q.cpu(), k.cpu(), v.cpu(), table.tolist(), [n], page, F32, blocks=blocks.tolist())
