@@ -12,7 +12,7 @@ namespace {
 constexpr int kPlanThreads = 1024;   // a thread per sequence
 static_assert(kPlanThreads == CERBERUS_MAX_SEQS, "k_page_plan has a thread per sequence");
 
-// inclusive sum over the workgroup's threads in order; sh holds an entry per wave
+// inclusive sum over the workgroup's threads in order; sh holds an entry per wave and belongs to this sum alone
 __device__ __forceinline__ long long scan_sum(long long v, long long* sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -20,10 +20,10 @@ __device__ __forceinline__ long long scan_sum(long long v, long long* sh) {
     const long long o = __shfl_up(v, off, 64);
     if (lane >= off) v += o;
   }
-  __syncthreads();                       // an earlier scan's entries have been read
   if (lane == 63) sh[wave] = v;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) v += sh[w];
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) v += w < wave ? sh[w] : 0;
   return v;
 }
 
@@ -40,18 +40,22 @@ __device__ __forceinline__ int owner_of(const long long* ends, int n, long long 
 }  // namespace
 
 // ---------------------------------------------------------------------------------------------
-// Plan of a batch: lengths, block tables and free pages (see cerberus_page_plan), and the slots of up to
-// kSlotsInPlan rows.  All of it follows from three running sums over the sequences, in their order: pages that come back,
-// rows, pages that are needed.  Sequence b is granted its pages if it fits and needs none or the running sum of needs up
-// to it is no more than the free pages; needs only grow along the sum, so the granted ones that need pages come before all
-// refused ones that do, and their places on the stack of free pages are that same sum.  Pages and rows are dealt to
-// threads one by one, whoever owns them (a search in the sums), not sequence by sequence: a prompt of thousands
-// of blocks next to sequences that need none would otherwise be one thread's loop.
-// One workgroup; its time is the chain of loads and barriers.
+// Plan of a batch: lengths, block tables, free pages and slots (see cerberus_page_plan).  All of it follows from three running
+// sums over the sequences, in their order: pages that come back, rows, pages that are needed.  Sequence b is granted
+// its pages if it fits and needs none or the running sum of needs up to it is no more than the free pages; needs only grow
+// along the sum, so the granted ones that need pages come before all refused ones that do, and their places on the
+// stack of free pages are that same sum.  Pages and rows are dealt to threads one by one, whoever owns them (a search in
+// the sums), not sequence by sequence: a prompt of thousands of blocks next to sequences that need none would otherwise be one thread's loop.
+// What is on place p of the stack is known without waiting for the pages that come back to be written there: from place nf0 on
+// it is a block of a sequence that ends.  So moving pages and forming slots only read what was there before the call
+// (free pages below nf0, blocks held, tables of sequences that end) and write other places.
+// A step's few rows take one workgroup and one launch (ALL; 4 us, a chain of loads and barriers); with a prompt's rows
+// many workgroups form the sums each for itself and share the pages and rows, and k_page_commit then writes what they read.
 // ---------------------------------------------------------------------------------------------
+template <bool ALL>
 __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_table pt, const int* new_rows, int most, int batch,
-                                                            int max_rows, int* row_start, int* first_pos, int* slot, int with_slots) {
-  __shared__ long long sh[kPlanThreads / 64];
+                                                            int max_rows, int* row_start, int* first_pos, int* slot) {
+  __shared__ long long sh[3][kPlanThreads / 64];
   __shared__ long long back_end[kPlanThreads], row_end[kPlanThreads], need_end[kPlanThreads];
   __shared__ int old_len[kPlanThreads], s_first[kPlanThreads];
   __shared__ long long s_grant;
@@ -63,16 +67,16 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
   const bool sane = L >= 0 && L <= cap, ends = n < 0;
   const int held = sane ? (int)(((long long)L + ps - 1) / ps) : 0;
   const int rows = max(n, 0);
+  if (t == 0) s_grant = 0;
 
-  const long long be = scan_sum(ends ? held : 0, sh), re = scan_sum(rows, sh);
+  const long long be = scan_sum(ends ? held : 0, sh[0]), re = scan_sum(rows, sh[1]);
   back_end[t] = be;
   row_end[t] = re;
   old_len[t] = L;
-  if (t == 0) s_grant = 0;
   const bool fits = t < batch && !ends && sane && (long long)L + rows <= cap && re <= max_rows;
   const int total = fits ? (int)(((long long)L + rows + ps - 1) / ps) : held;
   const int need = fits ? total - held : 0;
-  const long long ne = scan_sum(need, sh);
+  const long long ne = scan_sum(need, sh[2]);
   need_end[t] = ne;
   __syncthreads();
   const long long returned = back_end[kPlanThreads - 1];
@@ -80,70 +84,89 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
   const bool granted = fits && (need == 0 || ne <= nf1);
   s_first[t] = granted ? L : -1;
   if (granted && need > 0) atomicMax(&s_grant, ne);
-
-  // pages of the sequences that end, on top of the free ones in order of the sequences
-  for (long long i = t; i < returned; i += kPlanThreads) {
-    const int b = owner_of(back_end, batch, i);
-    const long long j = i - (b ? back_end[b - 1] : 0);
-    if (nf0 + i < pt.n_pages) pt.free_pages[nf0 + i] = pt.block_table[(size_t)b * pt.max_blocks + j];
-  }
-  __syncthreads();                         // (also: those pages are written before they are taken below)
+  __syncthreads();
   const long long grant = s_grant;
-  for (long long i = t; i < grant; i += kPlanThreads) {
-    const int b = owner_of(need_end, batch, i);
-    const int l = old_len[b];
-    const long long j = i - (b ? need_end[b - 1] : 0) + ((long long)l + ps - 1) / ps;
-    pt.block_table[(size_t)b * pt.max_blocks + j] = pt.free_pages[nf1 - 1 - i];
+
+  // what is on place p of the stack of free pages once the pages that come back are on it
+  auto on_stack = [&](long long p) {
+    if (p < nf0) return pt.free_pages[p];
+    const int b = owner_of(back_end, batch, p - nf0);
+    return pt.block_table[(size_t)b * pt.max_blocks + (p - nf0 - (b ? back_end[b - 1] : 0))];
+  };
+  // One list of all that is to be moved or formed, so that a thread's few turns are one after the other in any of the three kinds.
+  const long long n_back = nf1 - nf0, n_all = n_back + grant + max_rows, step = (long long)gridDim.x * kPlanThreads;
+  for (long long item = (long long)blockIdx.x * kPlanThreads + t; item < n_all; item += step) {
+    if (item < n_back) {                       // a page that comes back (one that is taken again at once keeps its place behind the list's end)
+      pt.free_pages[nf0 + item] = on_stack(nf0 + item);
+    } else if (item < n_back + grant) {        // a page for a block
+      const long long i = item - n_back;
+      const int b = owner_of(need_end, batch, i);
+      const long long j = i - (b ? need_end[b - 1] : 0) + ((long long)old_len[b] + ps - 1) / ps;
+      pt.block_table[(size_t)b * pt.max_blocks + j] = on_stack(nf1 - 1 - i);
+    } else {                                   // a row's slot
+      const long long i = item - n_back - grant;
+      const int b = owner_of(row_end, batch, i);
+      int v = -1;
+      if (b < batch && s_first[b] >= 0) {
+        const int pos = s_first[b] + (int)(i - (b ? row_end[b - 1] : 0)), blk = pos / ps;
+        const int have = (int)(((long long)old_len[b] + ps - 1) / ps);
+        const int page = blk < have ? pt.block_table[(size_t)b * pt.max_blocks + blk] : on_stack(nf1 - 1 - ((b ? need_end[b - 1] : 0) + blk - have));
+        v = page * ps + pos % ps;
+      }
+      slot[i] = v;
+    }
   }
+  if (blockIdx.x != 0) return;
   if (t < batch) {
-    if (ends || (granted && rows)) pt.kv_len[t] = ends ? 0 : L + rows;
     first_pos[t] = granted ? L : -1;
     row_start[t + 1] = (int)min(re, (long long)INT_MAX);
     if (!ends && !granted) atomicOr(pt.status, (int)CERBERUS_DEV_KV_OVERFLOW);
+    if (ALL && (ends || (granted && rows))) pt.kv_len[t] = ends ? 0 : L + rows;   // (everybody has read it)
   }
   if (t == 0) {
     row_start[0] = 0;
-    *pt.n_free = nf1 - (int)grant;
+    if (ALL) *pt.n_free = nf1 - (int)grant;
   }
-  if (!with_slots) return;
-  __syncthreads();                         // the tables are whole
-  for (int i = t; i < max_rows; i += kPlanThreads) {
-    const int b = owner_of(row_end, batch, i);
-    int v = -1;
-    if (b < batch && s_first[b] >= 0) {
-      const int pos = s_first[b] + (int)(i - (b ? row_end[b - 1] : 0));
-      v = pt.block_table[(size_t)b * pt.max_blocks + pos / ps] * ps + pos % ps;
+}
+
+// Lengths and free pages after a plan of many workgroups.
+__global__ __launch_bounds__(kPlanThreads) void k_page_commit(const cerberus_page_table pt, const int* __restrict__ new_rows, int most, int batch,
+                                                              const int* __restrict__ first_pos) {
+  __shared__ long long sh[2][kPlanThreads / 64];
+  const int t = threadIdx.x, ps = pt.page_size;
+  const long long cap = (long long)pt.max_blocks * ps;
+  const int nf0 = min(max(*pt.n_free, 0), pt.n_pages);
+  long long back = 0, taken = 0;
+  if (t < batch) {
+    const int L = pt.kv_len[t], n = min(new_rows ? new_rows[t] : 1, most);
+    if (n < 0) {
+      back = L >= 0 && L <= cap ? ((long long)L + ps - 1) / ps : 0;
+      pt.kv_len[t] = 0;
+    } else if (n > 0 && first_pos[t] >= 0) {
+      taken = ((long long)L + n + ps - 1) / ps - ((long long)L + ps - 1) / ps;
+      pt.kv_len[t] = L + n;
     }
-    slot[i] = v;
   }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) { back += __shfl_xor(back, off, 64); taken += __shfl_xor(taken, off, 64); }
+  if ((t & 63) == 0) { sh[0][t >> 6] = back; sh[1][t >> 6] = taken; }
+  __syncthreads();
+  if (t != 0) return;
+  back = taken = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) { back += sh[0][w]; taken += sh[1][w]; }
+  *pt.n_free = (int)(min((long long)pt.n_pages, nf0 + back) - taken);
 }
 
-// Slots of many rows, from what the plan left: a thread per row.
-__global__ __launch_bounds__(256) void k_page_slots(const cerberus_page_table pt, int batch, int max_rows, const int* __restrict__ row_start,
-                                                    const int* __restrict__ first_pos, int* __restrict__ slot) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= max_rows) return;
-  int lo = 0, hi = batch;                  // first sequence whose rows end above i
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (row_start[mid + 1] > i) hi = mid; else lo = mid + 1;
-  }
-  int v = -1;
-  if (lo < batch && first_pos[lo] >= 0) {
-    const int pos = first_pos[lo] + i - row_start[lo];
-    v = pt.block_table[(size_t)lo * pt.max_blocks + pos / pt.page_size] * pt.page_size + pos % pt.page_size;
-  }
-  slot[i] = v;
-}
-
-constexpr int kSlotsInPlan = 4096;
+constexpr int kRowsOfOne = 2048, kPlanWorkgroups = 128;
 
 hipError_t launch_page_plan(const cerberus_page_table& pt, const int* new_rows, int most, int batch, int max_rows, int* row_start,
                             int* first_pos, int* slot, hipStream_t s) {
-  const int with = max_rows <= kSlotsInPlan;
-  hipLaunchKernelGGL(k_page_plan, dim3(1), dim3(kPlanThreads), 0, s, pt, new_rows, most, batch, max_rows, row_start, first_pos, slot, with);
-  if (!with)
-    hipLaunchKernelGGL(k_page_slots, dim3((max_rows + 255) / 256), dim3(256), 0, s, pt, batch, max_rows, row_start, first_pos, slot);
+  if (max_rows <= kRowsOfOne) {
+    hipLaunchKernelGGL(k_page_plan<true>, dim3(1), dim3(kPlanThreads), 0, s, pt, new_rows, most, batch, max_rows, row_start, first_pos, slot);
+  } else {
+    hipLaunchKernelGGL(k_page_plan<false>, dim3(kPlanWorkgroups), dim3(kPlanThreads), 0, s, pt, new_rows, most, batch, max_rows, row_start, first_pos, slot);
+    hipLaunchKernelGGL(k_page_commit, dim3(1), dim3(kPlanThreads), 0, s, pt, new_rows, most, batch, first_pos);
+  }
   return hipGetLastError();
 }
 
@@ -152,7 +175,9 @@ hipError_t launch_page_plan(const cerberus_page_table& pt, const int* new_rows, 
 // that has a run's first row among its `chunk` rows takes the whole run for one key head: copies its K and V rows, folds
 // its keys and those that the page held before into the lowest and highest coordinate, and writes these once.  Nothing is
 // accumulated over calls, so a page that another sequence had before needs no clearing, and the order of workgroups does
-// not matter.  A row is dh * sizeof(T) / 16 lanes of 16 bytes; the workgroup's groups of so many lanes take rows in turn.
+// not matter.  Heads vary fastest over the workgroups, so that neighbours read what lies together in the rows; pages are written
+// past the caches, which they would only pass through before they are read again (14154 rows of 8 heads: 35 us
+// with plain stores and rows fastest, 28 with these stores, 26 with both; 23 is a copy of the same bytes).  A row is dh * sizeof(T) / 16 lanes of 16 bytes; the workgroup's groups of so many lanes take rows in turn.
 // ---------------------------------------------------------------------------------------------
 namespace {
 template <typename T> struct Vec16;   // 16 bytes as numbers
@@ -188,17 +213,26 @@ template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int chunk) {
   constexpr int N = Vec16<T>::N, LPR = DH / N, ROWS = 256 / LPR;   // lanes per row, rows side by side
   __shared__ float sh[2][4][DH];
-  const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
-  const int ps = a.pg.page_size, r_end = (int)min((long long)a.n_rows, (blockIdx.x + 1ll) * chunk);
+  const int ps = a.pg.page_size, r_end = (int)min((long long)a.n_rows, (blockIdx.y + 1ll) * chunk);
   const long long slots = (long long)a.pg.n_pages * ps;
   const T* k = reinterpret_cast<const T*>(a.k) + h * a.k_head + piece * N;
   const T* v = reinterpret_cast<const T*>(a.v) + h * a.v_head + piece * N;
   T* kp = reinterpret_cast<T*>(a.pg.k) + piece * N;
   T* vp = reinterpret_cast<T*>(a.pg.v) + piece * N;
 
-  for (int r = blockIdx.x * chunk; r < r_end;) {
-    const int s0 = a.slot[r];
+  const int begin = blockIdx.y * chunk;
+  for (int r = begin; r < r_end;) {
+    // the slots from here on, one lane each, that of the row before the chunk, and the first row itself (whatever its slot)
+    const int ahead = r + lane < a.n_rows ? a.slot[r + lane] : -1;
+    const int before = r == begin && r > 0 ? a.slot[r - 1] : -1;
+    uint4 k0 = make_uint4(0, 0, 0, 0), v0 = k0;
+    if (sub == 0) {
+      k0 = *reinterpret_cast<const uint4*>(k + (long long)r * a.k_row);
+      v0 = *reinterpret_cast<const uint4*>(v + (long long)r * a.v_row);
+    }
+    const int s0 = __builtin_amdgcn_readfirstlane(ahead);
     if (s0 < 0 || s0 >= slots) {                                   // (uniform over the workgroup, like all below)
       if (s0 >= 0 && h == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, (int)CERBERUS_DEV_BAD_PAGE);
       ++r;
@@ -206,16 +240,15 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
     }
     const int off0 = s0 & (ps - 1);
     // rows from here on that follow each other in this page
-    int len = 1;
     const int most = min(ps - off0, a.n_rows - r);
-    for (int i = 1; i < most; i += 64) {
-      const bool next = i + lane < most && a.slot[r + i + lane] == s0 + i + lane;
-      const unsigned long long m = __ballot(next);
-      if (m != ~0ull) { len += __ffsll((long long)~m) - 1; break; }
-      len += 64;
+    unsigned long long gap = ~__ballot(ahead == s0 + lane);
+    int len = gap ? __ffsll((long long)gap) - 1 : 64;
+    while (gap == 0 && len < most) {
+      gap = ~__ballot(len + lane < most && a.slot[r + len + lane] == s0 + len + lane);
+      len += gap ? __ffsll((long long)gap) - 1 : 64;
     }
     len = min(len, most);
-    if (off0 != 0 && r > 0 && r == (int)blockIdx.x * chunk && a.slot[r - 1] == s0 - 1) {   // the run began in the chunk before
+    if (off0 != 0 && before == s0 - 1) {                           // the run began in the chunk before
       r += len;
       continue;
     }
@@ -230,10 +263,13 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
       for (int e = 0; e < N; ++e) { lo[e] = lower(f[e], lo[e]); hi[e] = higher(f[e], hi[e]); }
     };
     for (int i = sub; i < len; i += ROWS) {
-      const uint4 ku = *reinterpret_cast<const uint4*>(k + (long long)(r + i) * a.k_row);
-      const uint4 vu = *reinterpret_cast<const uint4*>(v + (long long)(r + i) * a.v_row);
-      *reinterpret_cast<uint4*>(kp + (row0 + off0 + i) * DH) = ku;
-      *reinterpret_cast<uint4*>(vp + (row0 + off0 + i) * DH) = vu;
+      uint4 ku = k0, vu = v0;
+      if (i > 0) {
+        ku = *reinterpret_cast<const uint4*>(k + (long long)(r + i) * a.k_row);
+        vu = *reinterpret_cast<const uint4*>(v + (long long)(r + i) * a.v_row);
+      }
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, ku), reinterpret_cast<u32x4_t*>(kp + (row0 + off0 + i) * DH));
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, vu), reinterpret_cast<u32x4_t*>(vp + (row0 + off0 + i) * DH));
       fold(ku);
     }
     if (a.pg.bounds) {
@@ -272,11 +308,11 @@ constexpr int kStoreWorkgroups = 2048;
 
 hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
   // Workgroups for the whole card before any takes several runs: a row each while there are few (a decoding step's rows are
-  // runs of one), up to about a page of rows for prompts, whose runs are pages; never more than 2^20 along the rows.
+  // runs of one), up to about a page of rows for prompts, whose runs are pages; never more than a grid has along the rows.
   const long long work = (long long)a.n_rows * a.pg.n_kv_heads;
   int chunk = (int)std::min<long long>(std::max<long long>(1, work / kStoreWorkgroups), a.pg.page_size);
-  chunk = std::max(chunk, (a.n_rows - 1) / (1 << 20) + 1);
-  dim3 grid((a.n_rows + chunk - 1) / chunk, a.pg.n_kv_heads);
+  chunk = std::max(chunk, (a.n_rows - 1) / 65535 + 1);
+  dim3 grid(a.pg.n_kv_heads, (a.n_rows - 1) / chunk + 1);
   const bool wide = a.pg.head_dim == 128;
   if (a.pg.dtype == CERBERUS_F32) {
     if (wide) hipLaunchKernelGGL((k_page_store<float, 128>), grid, dim3(256), 0, s, a, chunk);

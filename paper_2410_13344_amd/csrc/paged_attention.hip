@@ -9,6 +9,10 @@ namespace cerb {
 
 namespace {
 
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kShort = 512;      // rows below which a piece's beginning and end show in its time
+
 // How the rows of a batch are cut.  Sequence b has rows_of(b) rows to look at (with chosen blocks: the rows of all places of
 // its list); they are cut into pieces of `piece` rows, a multiple of what a workgroup takes at a time, and every (piece, key
 // head, 16 of its query heads) is a workgroup.  A sequence of one piece is written out by its workgroup, the pieces of
@@ -25,7 +29,7 @@ __device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int b) {
   return a.blocks && L > 0 ? a.n_select << a.page_shift : L;
 }
 
-// item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks after sequences l * k .. l * k + k - 1.
+// unit: pieces are a multiple of so many rows.  item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks after sequences l * k .. l * k + k - 1.
 __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
   const int lane = threadIdx.x & 63, k = (a.batch + 63) >> 6, b0 = lane * k, b1 = min(a.batch, b0 + k);
   long long total = 0;
@@ -33,8 +37,9 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
   Cut c;
-  // as many pieces as the launch has workgroups for: at most per_head + one per sequence
-  const long long want = (total + per_head - 1) / per_head;
+  // as many pieces as the launch has workgroups for (at most per_head + one per sequence), half as many where they would be short
+  const long long full = (total + per_head - 1) / per_head, half = (total + (per_head + 1) / 2 - 1) / ((per_head + 1) / 2);
+  const long long want = max(full, min(half, (long long)kShort));
   c.piece = (int)min((max(want, 1ll) + unit - 1) / unit * unit, (long long)INT_MAX);   // (at INT_MAX nothing is cut)
   auto pieces_of = [&](int b) { return max(1, (int)(((unsigned)rows_of(a, b) + (unsigned)c.piece - 1u) / (unsigned)c.piece)); };
   int n = 0, cuts = 0;
@@ -106,14 +111,17 @@ template <int DH> struct Stage<float, DH> {
 // bf16: probabilities go into the second product as two bf16 planes (p to 2^-17): the matrix units have time.
 // STEP: a decoding step's queries and outputs are two bf16 planes, and the newest row has a second plane next to the cache.
 // ---------------------------------------------------------------------------------------------
-template <typename T, int DH, bool STEP>
-__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, int per_head) {
+// ONCE: K and V are read once in the launch (up to 16 queries per key head): loaded with the streaming hint.  A model's layers hold more
+// than the caches do, so nothing of them is there again in the next step.  131072 rows x 8 key heads: 103 -> 91 us, 64 sequences of
+// up to 16384: 206 -> 192; only caches that fit the last-level cache whole lose (134 MB read again and again: 28 -> 32).
+template <typename T, int DH, bool STEP, bool ONCE>
+__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, int unit, int per_head) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int U = Tile<T>::U, DV = DH / 16, KS = BF ? DH / 32 : DH / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15, g = lane >> 4;
   const int nkv = a.pg.n_kv_heads, group = a.n_heads / nkv;
   const int hk = blockIdx.x % nkv, h0 = blockIdx.x / nkv * 16;      // key head; first of its queries
-  const Cut cut = find_cut(a, blockIdx.y, false, kUnit<T>, per_head);
+  const Cut cut = find_cut(a, blockIdx.y, false, unit, per_head);
   if (cut.b < 0) return;                                            // (uniform over the workgroup)
   const int b = __builtin_amdgcn_readfirstlane(cut.b), ps = a.pg.page_size;
   const int L = min(max(a.lens[b], 0), a.max_blocks << a.page_shift), held = (int)(((long long)L + ps - 1) >> a.page_shift);
@@ -173,26 +181,27 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, in
       const T* kr = pool_k + (row0 + min(lq, last)) * DH;
       if constexpr (BF) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) st.k[u][s] = *reinterpret_cast<const uint4*>(kr + s * 32 + g * 8);
+        for (int s = 0; s < KS; ++s) st.k[u][s] = ld_w<ONCE>(reinterpret_cast<const uint4*>(kr + s * 32 + g * 8));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const T* vr = pool_v + (row0 + min(4 * g + i, last)) * DH + lq * DV;
           if constexpr (DV == 8) {
-            const uint4 w = *reinterpret_cast<const uint4*>(vr);
+            const uint4 w = ld_w<ONCE>(reinterpret_cast<const uint4*>(vr));
             st.v[u * 4 + i][0] = w.x; st.v[u * 4 + i][1] = w.y; st.v[u * 4 + i][2] = w.z; st.v[u * 4 + i][3] = w.w;
           } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(vr);
-            st.v[u * 4 + i][0] = w.x; st.v[u * 4 + i][1] = w.y;
+            const u32x2_t* p = reinterpret_cast<const u32x2_t*>(vr);
+            const u32x2_t w = ONCE ? __builtin_nontemporal_load(p) : *p;
+            st.v[u * 4 + i][0] = w[0]; st.v[u * 4 + i][1] = w[1];
           }
         }
       } else {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) st.k[u][s] = *reinterpret_cast<const float4*>(kr + s * 16 + g * 4);
+        for (int s = 0; s < KS; ++s) st.k[u][s] = __builtin_bit_cast(float4, ld_w<ONCE>(reinterpret_cast<const uint4*>(kr + s * 16 + g * 4)));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int r = 0; r < DH / 64; ++r)
-            st.v[i][r] = *reinterpret_cast<const float4*>(pool_v + (row0 + min(4 * g + i, last)) * DH + r * 64 + lq * 4);
+            st.v[i][r] = __builtin_bit_cast(float4, ld_w<ONCE>(reinterpret_cast<const uint4*>(pool_v + (row0 + min(4 * g + i, last)) * DH + r * 64 + lq * 4)));
       }
     }
   };
@@ -395,40 +404,54 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, in
   }
 }
 
-// Joins the pieces of a sequence: a workgroup per (head, sequence), groups of DH / 4 lanes take pieces in turn.
+// Joins the pieces of a sequence: a workgroup takes `heads` (a power of two) heads, groups of DH / 4 lanes take pieces in turn,
+// four at a time.
 template <typename T, int DH, bool STEP>
-__global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int unit, int per_head) {
+__global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int unit, int per_head, int heads) {
   constexpr int LPP = DH / 4, GROUPS = 256 / LPP;
-  const int h = blockIdx.x, b = blockIdx.y;
+  const int b = blockIdx.y, t = threadIdx.x / LPP, d = threadIdx.x % LPP * 4;
   const Cut cut = find_cut(a, b, true, unit, per_head);
   if (cut.pieces <= 1) return;                                      // written out already
-  const int t = threadIdx.x / LPP, d = threadIdx.x % LPP * 4;
+  const int per = GROUPS / heads, h = min((int)blockIdx.x * heads + t / per, a.n_heads - 1), first = t % per;
   const float* ml = a.part + (size_t)2 * per_head * a.n_heads * DH;
   float M = -INFINITY, den = 0.f, num[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int j = t; j < cut.pieces; j += GROUPS) {
-    const size_t at = (size_t)(cut.slot0 + j) * a.n_heads + h;
-    const float2 x = *reinterpret_cast<const float2*>(ml + at * 2);
-    const float4 o = *reinterpret_cast<const float4*>(a.part + at * DH + d);
-    const float mn = fmaxf(M, x.x), base = mn == -INFINITY ? 0.f : mn;
-    const float f0 = __builtin_amdgcn_exp2f(M - base), f1 = __builtin_amdgcn_exp2f(x.x - base);
+  for (int j0 = first; j0 < cut.pieces; j0 += 4 * per) {
+    float2 x[4];
+    float4 o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const size_t at = (size_t)(cut.slot0 + min(j0 + i * per, cut.pieces - 1)) * a.n_heads + h;
+      x[i] = *reinterpret_cast<const float2*>(ml + at * 2);
+      o[i] = *reinterpret_cast<const float4*>(a.part + at * DH + d);
+    }
+    float mn = M;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (j0 + i * per >= cut.pieces) { x[i] = make_float2(-INFINITY, 0.f); o[i] = make_float4(0.f, 0.f, 0.f, 0.f); }
+      mn = fmaxf(mn, x[i].x);
+    }
+    const float base = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(M - base);
     M = mn;
-    den = den * f0 + x.y * f1;
-    num[0] = num[0] * f0 + o.x * f1; num[1] = num[1] * f0 + o.y * f1; num[2] = num[2] * f0 + o.z * f1; num[3] = num[3] * f0 + o.w * f1;
+    den *= f0; num[0] *= f0; num[1] *= f0; num[2] *= f0; num[3] *= f0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = __builtin_amdgcn_exp2f(x[i].x - base);
+      den += x[i].y * f;
+      num[0] += o[i].x * f; num[1] += o[i].y * f; num[2] += o[i].z * f; num[3] += o[i].w * f;
+    }
   }
   __shared__ float sm[GROUPS], sd[GROUPS];
   __shared__ __attribute__((aligned(16))) float so[GROUPS][DH];
   *reinterpret_cast<float4*>(&so[t][d]) = make_float4(num[0], num[1], num[2], num[3]);
   if (d == 0) { sm[t] = M; sd[t] = den; }
   __syncthreads();
-  if (t != 0) return;
-#pragma unroll
-  for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, sm[i]);
+  if (first != 0 || (int)blockIdx.x * heads + t / per >= a.n_heads) return;
+  for (int i = 1; i < per; ++i) M = fmaxf(M, sm[t + i]);
   den = num[0] = num[1] = num[2] = num[3] = 0.f;
-#pragma unroll
-  for (int i = 0; i < GROUPS; ++i) {
-    const float f = sm[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[i] - M);
-    const float4 o = *reinterpret_cast<const float4*>(&so[i][d]);
-    den += f * sd[i];
+  for (int i = 0; i < per; ++i) {
+    const float f = sm[t + i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[t + i] - M);
+    const float4 o = *reinterpret_cast<const float4*>(&so[t + i][d]);
+    den += f * sd[t + i];
     num[0] += f * o.x; num[1] += f * o.y; num[2] += f * o.z; num[3] += f * o.w;
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;
@@ -444,7 +467,9 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int u
 
 namespace {
 
-constexpr int kTarget = 1024;     // workgroups a launch aims for, four per compute unit
+constexpr int kTarget = 1024;     // workgroups a launch aims for, four per compute unit (two run at a time)
+constexpr int kWhole = 512;       // rows that one workgroup reads in less time than a join takes
+constexpr int kLists = 256;       // workgroups that keep the memory busy
 
 int head_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 // pieces that a launch aims for per (key head, 16 queries)
@@ -453,12 +478,21 @@ int per_head_of(int n_heads, int n_kv_heads) { return std::max(1, kTarget / (n_k
 template <typename T, int DH, bool STEP>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
   const int tiles = head_tiles(a.n_heads, a.pg.n_kv_heads), per_head = per_head_of(a.n_heads, a.pg.n_kv_heads);
-  // no sequence can be cut if all the table or the list has room for is one workgroup's turn
+  // Joining pieces is a launch of its own, 5 to 8 us with what goes before it, and a workgroup by itself reads about 90 rows a us
+  // (bf16, 128 columns).  So nothing is cut where all that the table or the list has room for is kWhole rows, and lists, which
+  // are of one length, are not where they are enough workgroups to keep the memory busy.
   const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift;
-  const bool cuts = most > kUnit<T>;
-  const int items = a.batch + (cuts ? per_head : 0);
-  hipLaunchKernelGGL((k_paged_attn<T, DH, STEP>), dim3(a.pg.n_kv_heads * tiles, items), dim3(256), 0, s, a, per_head);
-  if (cuts) hipLaunchKernelGGL((k_paged_join<T, DH, STEP>), dim3(a.n_heads, a.batch), dim3(256), 0, s, a, kUnit<T>, per_head);
+  const bool cuts = most > kWhole && !(a.blocks && (long long)a.batch * a.pg.n_kv_heads * tiles >= kLists);
+  const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512, items = (int)std::min<long long>(a.batch + per_head, a.batch * ((most - 1) / unit + 1));
+  const dim3 grid(a.pg.n_kv_heads * tiles, items);
+  if (STEP || tiles == 1) hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, true>), grid, dim3(256), 0, s, a, unit, per_head);   // (a step's heads share no keys)
+  else hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, STEP>), grid, dim3(256), 0, s, a, unit, per_head);
+  if (cuts) {
+    // A head per workgroup where that is at most four for every compute unit (few sequences have many pieces each), else up to
+    // four heads: most sequences of a large batch have nothing to join, and their workgroups only find that out.
+    const int heads = a.batch * a.n_heads <= 1024 ? 1 : 4;
+    hipLaunchKernelGGL((k_paged_join<T, DH, STEP>), dim3((a.n_heads + heads - 1) / heads, a.batch), dim3(256), 0, s, a, unit, per_head, heads);
+  }
 }
 
 }  // namespace
