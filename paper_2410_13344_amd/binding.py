@@ -342,7 +342,7 @@ class PagePlan:
 
 class PageCache:
     """A key-value cache in pages that up to max_seqs sequences share: the device arrays of a cerberus_page_table and of the
-    cerberus_pages of n_layers layers, and the workspace of the calls on them.  max_blocks: blocks of a sequence at most.  The
+    cerberus_pages of n_layers layers.  max_blocks: blocks of a sequence at most.  The
     bookkeeping (free pages, status, lengths, tables) is one tensor, `words`: a copy of it is a snapshot of who owns which page.
     A call on another stream than torch's current one of the cache's device: pass it as `stream`, and order the streams as for
     any tensor.  Outputs and workspaces come from torch's allocator per call, on the call's stream, so calls on
@@ -540,11 +540,15 @@ class Engine:
                stream=None):
         cerberus_decode(self.ctx, st.struct, batch, n_steps, out_tokens, out_count, stream)
 
+    def _fits(self, st: DeviceState, cache: PageCache) -> None:
+        if cache.n_layers != self.cfg["n_layers"] or cache.device != st.kv.device or cache.dtype != st.kv.dtype or \
+                cache.n_kv_heads != self.cfg["n_heads"] or cache.head_dim != self.cfg["head_dim"]:
+            raise ValueError("a page cache of another model, dtype or device")
+
     def paged_step(self, st: DeviceState, cache: PageCache, batch: int, new_rows: Optional[torch.Tensor] = None, n_select: int = 0,
                    stream=None):
         """ar_step with the cache in pages: new_rows[b] 1 decodes a token, 0 sits out, below 0 ends the sequence."""
-        if cache.n_layers != self.cfg["n_layers"]:
-            raise ValueError("a page cache of another number of layers than the model")
+        self._fits(st, cache)
         if new_rows is not None:
             cache._ints("new_rows", new_rows, (batch,))
         nbytes = cache.workspace_bytes(batch, self.cfg["n_heads"], n_select)
@@ -555,8 +559,8 @@ class Engine:
     def move_prompts(self, st: DeviceState, cache: PageCache, lens: Sequence[int], stream=None) -> PagePlan:
         """Rows 0..lens[b]-1 of the slab's sequences (0: none) become the next rows of the page cache's: what a prompt phase
         leaves goes on in pages, and the slab's places are free for other prompts."""
-        if cache.n_layers != self.cfg["n_layers"] or not 1 <= len(lens) <= min(cache.max_seqs, self.max_batch) or \
-                min(lens) < 0 or max(lens) > self.kv_capacity:
+        self._fits(st, cache)
+        if not 1 <= len(lens) <= min(cache.max_seqs, self.max_batch) or min(lens) < 0 or max(lens) > self.kv_capacity:
             raise ValueError("lens do not fit the slab or the page cache")
         with cache._on(stream):
             plan = cache.plan(torch.tensor(lens, dtype=torch.int32, device=cache.device), sum(lens))
@@ -570,9 +574,14 @@ class Engine:
 
     def generate_paged(self, st: DeviceState, cache: PageCache, prompts, n_steps: int, n_select: int = 0, stream=None):
         """Prompt phase in the slab, then n_steps one-token steps in pages; returns the committed token ids of every sequence
-        (fewer where the pages ran out) and ends the sequences."""
+        (fewer where the pages ran out) and ends the sequences, the first of the cache: they must be empty."""
         batch = len(prompts)
+        self._fits(st, cache)
+        if not 1 <= batch <= min(cache.max_seqs, self.max_batch) or max(len(p) for p in prompts) > self.kv_capacity:
+            raise ValueError("prompts do not fit the slab or the page cache")
         with cache._on(stream):
+            if cache.kv_len[:batch].any():
+                raise ValueError("the page cache's sequences are not empty")
             st.kv_len[:batch] = 0
             for b, p in enumerate(prompts):
                 self.prefill(st, batch, b, p.to(device="cuda", dtype=torch.int32))

@@ -115,13 +115,17 @@ template <int DH> struct Stage<float, DH> {
 // than the caches do, so nothing of them is there again in the next step.  131072 rows x 8 key heads: 103 -> 91 us, 64 sequences of
 // up to 16384: 206 -> 192; only caches that fit the last-level cache whole lose (134 MB read again and again: 28 -> 32).
 template <typename T, int DH, bool STEP, bool ONCE>
-__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, int unit, int per_head) {
+__global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, int unit, int per_head, int tiles, int items) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int U = Tile<T>::U, DV = DH / 16, KS = BF ? DH / 32 : DH / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15, g = lane >> 4;
   const int nkv = a.pg.n_kv_heads, group = a.n_heads / nkv;
-  const int hk = blockIdx.x % nkv, h0 = blockIdx.x / nkv * 16;      // key head; first of its queries
-  const Cut cut = find_cut(a, blockIdx.y, false, unit, per_head);
+  // Workgroups in order of pieces, key heads, tiles of 16 queries; consecutive ones go to the 8 XCDs in turn, so the tiles of
+  // one (piece, key head), which read the same rows, are 8 apart and meet in one L2.
+  const long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x, pair = id / (8 * tiles) * 8 + id % 8;
+  const int item = (int)(pair / nkv), hk = (int)(pair % nkv), h0 = (int)(id / 8 % tiles) * 16;   // piece, key head, first of its queries
+  if (item >= items) return;
+  const Cut cut = find_cut(a, item, false, unit, per_head);
   if (cut.b < 0) return;                                            // (uniform over the workgroup)
   const int b = __builtin_amdgcn_readfirstlane(cut.b), ps = a.pg.page_size;
   const int L = min(max(a.lens[b], 0), a.max_blocks << a.page_shift), held = (int)(((long long)L + ps - 1) >> a.page_shift);
@@ -484,9 +488,10 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
   const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift;
   const bool cuts = most > kWhole && !(a.blocks && (long long)a.batch * a.pg.n_kv_heads * tiles >= kLists);
   const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512, items = (int)std::min<long long>(a.batch + per_head, a.batch * ((most - 1) / unit + 1));
-  const dim3 grid(a.pg.n_kv_heads * tiles, items);
-  if (STEP || tiles == 1) hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, true>), grid, dim3(256), 0, s, a, unit, per_head);   // (a step's heads share no keys)
-  else hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, STEP>), grid, dim3(256), 0, s, a, unit, per_head);
+  const long long all = ((long long)items * a.pg.n_kv_heads + 7) / 8 * 8 * tiles, row = std::max(8ll * tiles, (1ll << 18) / (8 * tiles) * (8 * tiles));
+  const dim3 grid((unsigned)std::min(all, row), (unsigned)((all - 1) / row + 1));
+  if (STEP || tiles == 1) hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, true>), grid, dim3(256), 0, s, a, unit, per_head, tiles, items);   // (a step's heads share no keys)
+  else hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, STEP>), grid, dim3(256), 0, s, a, unit, per_head, tiles, items);
   if (cuts) {
     // A head per workgroup where that is at most four for every compute unit (few sequences have many pieces each), else up to
     // four heads: most sequences of a large batch have nothing to join, and their workgroups only find that out.

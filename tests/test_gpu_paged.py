@@ -450,6 +450,15 @@ def test_attention_past_32_bits_of_offset():
     assert torch.equal(c.bounds[0, 139999, :, 0].cpu(), k[at[139999]].amin(1))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_of_many_heads_and_key_heads(dtype):
+    """Head layouts that leave the last group of eight workgroups, or of sixteen queries, part empty."""
+    lens = [700, 33, 0, 129]
+    for heads, kv in ((1, 1), (3, 3), (9, 9), (35, 1), (66, 2), (51, 3), (70, 7)):
+        c, k, v, table, q = filled(dtype, heads, kv, 64, 16, lens, seed=heads)
+        check_attention(c.attention(0, q.cuda()), q, k, v, table, lens, 16, dtype)
+
+
 def test_attention_gives_the_same_bits_again():
     c, k, v, table, q = filled(BF16, 8, 2, 128, 16, [4000, 17, 900])
     d = q.cuda()
@@ -712,10 +721,27 @@ def test_paged_step_sits_out_ends_and_runs_out_of_pages(dtype):
     eng.paged_step(sp, cache, 3, torch.tensor([-1, 1, 1], dtype=torch.int32, device="cuda"))
     assert sp.accept_len.tolist() == [0, 1, 1] and cache.kv_len.tolist() == [0, 17, 21] and int(cache.status) == 0
     assert int(cache.n_free) == 1 and int(sp.accepted_tokens[1, 0]) == int(root[1])
+    other = F32 if dtype == BF16 else BF16
+    for bad in (B.PageCache(1, 5, 16, 4, 64, dtype, 3, 3), B.PageCache(cfg["n_layers"], 5, 16, 2, 64, dtype, 3, 3),
+                B.PageCache(cfg["n_layers"], 5, 16, 4, 64, other, 3, 3)):
+        with pytest.raises(ValueError):
+            eng.paged_step(sp, bad, 3)
+        with pytest.raises(ValueError):
+            eng.move_prompts(sp, bad, [1, 1, 1])
+    for lens_bad in ([1] * 4, [193], [-1], []):
+        with pytest.raises(ValueError):
+            eng.move_prompts(sp, cache, lens_bad)
     with pytest.raises(ValueError):
-        eng.paged_step(sp, B.PageCache(1, 5, 16, 4, 64, dtype, 3, 3), 3)
-    with pytest.raises(B.CerberusError):
-        eng.paged_step(sp, B.PageCache(cfg["n_layers"], 5, 16, 2, 64, dtype, 3, 3), 3)
+        eng.generate_paged(sp, cache, _prompts(cfg, [5, 5]), 1)                              # the second holds rows
+    pages, table = cache.layers, cache.table                                                 # and from C
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    wrong = (B.Pages * 2)(*[B.Pages(p.k, p.v, p.bounds, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, 1 - dtype) for p in pages])
+    with pytest.raises(B.CerberusError, match="layer 0"):
+        B.cerberus_paged_step(eng.ctx, sp.struct, wrong, table, 3, None, 0, ws)
+    with pytest.raises(B.CerberusError, match="batch"):
+        B.cerberus_paged_step(eng.ctx, sp.struct, pages, table, 4, None, 0, ws)
+    with pytest.raises(B.CerberusError, match="workspace"):
+        B.cerberus_paged_step(eng.ctx, sp.struct, pages, table, 3, None, 0, ws[:256])
     with pytest.raises(B.CerberusError):
         eng.paged_step(sp, cache, 3, n_select=2)                                              # without bounds
     pair.engine.close()
