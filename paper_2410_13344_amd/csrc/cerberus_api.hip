@@ -624,12 +624,17 @@ int run_gemm(const cerberus_ctx* c, const GemmBatch& plan, const int* n_rows, in
     if (rc_ != CERBERUS_OK) return rc_; \
   } while (0)
 
-// whole-K fused launches of layer l over the rows of the current row map (kv_layer may be null: no cache write)
-int run_fused_qkv(const cerberus_ctx* c, int l, void* kv_layer, hipStream_t s) {
+// The slab's rows of one layer (null: nowhere)
+CacheRows slab_rows(const Dims& D, void* kv_layer, int elem) {
+  return CacheRows{kv_layer, kv_layer ? (unsigned char*)kv_layer + (size_t)D.Bmax * D.nH * D.cap * D.dh * elem : nullptr, (size_t)D.cap * D.dh, nullptr, 0};
+}
+
+// whole-K fused launches of layer l over the rows of the current row map (cache.k may be null: no cache write)
+int run_fused_qkv(const cerberus_ctx* c, int l, const CacheRows& cache, hipStream_t s) {
   const Dims& D = c->D;
   FusedQkvArgs fa{};
   fa.W = c->st_qkv[l]; fa.At = c->xn; fa.slabs = c->slabs_qkv; fa.ksteps = kpad(c->cfg, D.d) / 32; fa.ssq = c->ssq;
-  fa.nb = add_gain_blocks(D.d, A_FRAG64); fa.rope_cs = c->rope_cs; fa.rm = c->rm; fa.q = (bf16_t*)c->q; fa.kv_layer = (bf16_t*)kv_layer;
+  fa.nb = add_gain_blocks(D.d, A_FRAG64); fa.rope_cs = c->rope_cs; fa.rm = c->rm; fa.q = (bf16_t*)c->q; fa.cache = cache;
   fa.ktree = (bf16_t*)c->ktree; fa.vtree = (bf16_t*)c->vtree; fa.lo_off = (size_t)c->R64 * D.d; fa.D = D;
   HIP_TRY(launch_qkv_rope(fa, c->ns_qkv, c->fused_grid, s));
   return CERBERUS_OK;
@@ -662,10 +667,10 @@ bool tile_launches(const cerberus_ctx* c, int rows_max, int above) {
 bool act_frag(const cerberus_ctx* c, int rows_max) { return tile_launches(c, rows_max, kTileAll) && c->D.F == c->D.Fpad; }
 
 // n_rows of the three: the device row count, or null for rows_max rows
-int run_tile_qkv(const cerberus_ctx* c, int l, void* kv_layer, const int* n_rows, int rows_max, hipStream_t s) {
+int run_tile_qkv(const cerberus_ctx* c, int l, const CacheRows& cache, const int* n_rows, int rows_max, hipStream_t s) {
   const Dims& D = c->D;
   FusedQkvArgs fa{};
-  fa.ssq = c->ssq; fa.nb = add_gain_blocks(D.d, A_FRAG); fa.rope_cs = c->rope_cs; fa.rm = c->rm; fa.q = (bf16_t*)c->q; fa.kv_layer = (bf16_t*)kv_layer;
+  fa.ssq = c->ssq; fa.nb = add_gain_blocks(D.d, A_FRAG); fa.rope_cs = c->rope_cs; fa.rm = c->rm; fa.q = (bf16_t*)c->q; fa.cache = cache;
   fa.ktree = (bf16_t*)c->ktree; fa.vtree = (bf16_t*)c->vtree; fa.lo_off = (size_t)c->R64 * D.d; fa.D = D;
   const TileGemmArgs ta{c->wqkv[l], c->xn, kpad(c->cfg, D.d) / 32, 3 * D.d / 32, n_rows, rows_max};
   HIP_TRY(launch_tile_qkv(ta, fa, c->fused_grid, s));
@@ -714,15 +719,24 @@ struct PagedStep {
   int n_select;
 };
 
-// Layer l's new rows (row b: sequence b) go to their slots, then each attends to its sequence's pages
+// Layer l's pages as the QKV projection writes its rows to them.  Where the pages keep bounds it does not: the store that forms
+// them writes the rows.  (A store by itself is 6 us a layer, 5 % of a 7B step of one sequence.)
+CacheRows page_rows(const Dims& D, const PagedStep& pp, int l) {
+  const cerberus_pages& pg = pp.layers[l];
+  return pg.bounds ? CacheRows{} : CacheRows{pg.k, pg.v, (size_t)pg.page_size * D.dh, pp.ws.slot, page_shift_of(pg.page_size)};
+}
+
+// Layer l's new rows (row b: sequence b) go to their slots, if they are not there yet, then each attends to its sequence's pages
 int run_paged_attention(const cerberus_ctx* c, const PagedStep& pp, int l, int batch, hipStream_t s) {
   const Dims& D = c->D;
   const bool bf16 = D.dtype == CERBERUS_BF16;
   const size_t lo = (size_t)c->R64 * D.d;
   const int shift = page_shift_of(pp.pt->page_size);
-  const void *k = bf16 ? c->ktree : pp.ws.k_rows, *v = bf16 ? c->vtree : pp.ws.v_rows;
   const cerberus_pages& pg = pp.layers[l];
-  HIP_TRY(launch_page_store(PageStoreArgs{pg, k, v, D.d, D.dh, D.d, D.dh, pp.ws.slot, batch, shift, pp.pt->status}, s));
+  if (pg.bounds) {
+    const void *k = bf16 ? c->ktree : pp.ws.k_rows, *v = bf16 ? c->vtree : pp.ws.v_rows;
+    HIP_TRY(launch_page_store(PageStoreArgs{pg, k, v, D.d, D.dh, D.d, D.dh, pp.ws.slot, batch, shift, pp.pt->status}, s));
+  }
   if (pp.n_select) {
     PageSelectArgs a{};
     a.pg = pg; a.table = pp.pt->block_table; a.lens = pp.ws.lens; a.max_blocks = pp.pt->max_blocks; a.page_shift = shift;
@@ -763,14 +777,15 @@ int forward_rows(cerberus_ctx* c, const cerberus_state* st, int rows_max, const 
                             prev ? (size_t)prev->out_rows * prev->N : 0, c->attn_norm[l], c->xn, c->ssq, rows_max, s, fq ? A_FRAG64 : tq ? A_FRAG : A_ROWS));
     GemmProb pq, po, pg;
     void* kv_layer = pages ? nullptr : (unsigned char*)st->kv + (size_t)l * kv_layer_bytes;
+    const CacheRows cache = pages ? page_rows(D, *pages, l) : slab_rows(D, kv_layer, c->elem);
     if (fq) {
-      TRY(run_fused_qkv(c, l, kv_layer, s));
+      TRY(run_fused_qkv(c, l, cache, s));
     } else if (tq) {
-      TRY(run_tile_qkv(c, l, kv_layer, rm.n_rows, rows_max, s));
+      TRY(run_tile_qkv(c, l, cache, rm.n_rows, rows_max, s));
     } else {
       TRY(run_gemm(c, c->p_qkv[l], rm.n_rows, 0, rows_max, nullptr, 0, s, &pq, qkv_split));
       const bool rows = pages && D.dtype == CERBERUS_F32;   // (bf16 mode has planes of the new rows anyway)
-      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, kv_layer, rows ? pages->ws.k_rows : c->ktree,
+      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, cache, rows ? pages->ws.k_rows : c->ktree,
                              rows ? pages->ws.v_rows : c->vtree, c->ssq, rows_max, s));
     }
     if (pages) {
@@ -880,7 +895,7 @@ int run_paged_step(cerberus_ctx* c, const cerberus_state* st, const PagedStep& p
   in_pages.kv = nullptr;
   in_pages.kv_len = pp.pt->kv_len;          // (the acceptance writes the length that the plan has put there already)
   HIP_TRY(launch_page_plan(*pp.pt, new_rows, 1, batch, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, s));
-  HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
+  HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, *pp.pt, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
   GemmProb pd{};
   TRY(forward_rows(c, &in_pages, batch, c->tree, AttnShape{1, batch, 0, 0}, &pd, s, &pp));
   TRY(run_lm_head(c, pd, nullptr, batch, s));
@@ -1217,7 +1232,7 @@ int cerberus_bench_gemm(cerberus_ctx* ctx, int32_t kind, int32_t rows, void* str
   if (kind == 0 && fused && ctx->ns_qkv) {
     // what a step of this many rows launches for the QKV projection: the whole-K kernel with its RoPE
     // epilogue, over the rows of the last step's row map (which must hold `rows` rows), minus the cache write
-    for (int l = 0; l < D.n_layers; ++l) TRY(run_fused_qkv(ctx, l, nullptr, s));
+    for (int l = 0; l < D.n_layers; ++l) TRY(run_fused_qkv(ctx, l, CacheRows{}, s));
     total = (double)D.n_layers * ((double)3 * D.d * D.d + (double)rows * D.d * 2) * ctx->elem;
   } else if (kind == 2 && fused && ctx->ns_gu) {
     for (int l = 0; l < D.n_layers; ++l) TRY(run_fused_gate_up(ctx, l, s));
@@ -1228,7 +1243,7 @@ int cerberus_bench_gemm(cerberus_ctx* ctx, int32_t kind, int32_t rows, void* str
     const GemmProb& P = (kind == 0 ? ctx->p_qkv : kind == 1 ? ctx->p_o : kind == 2 ? ctx->p_gu : ctx->p_down)[0].p[0];
     GemmProb launched;
     for (int l = 0; l < D.n_layers; ++l) {
-      if (kind == 0) TRY(run_tile_qkv(ctx, l, nullptr, nullptr, rows, s));
+      if (kind == 0) TRY(run_tile_qkv(ctx, l, CacheRows{}, nullptr, rows, s));
       else if (kind == 2) TRY(run_tile_gate_up(ctx, l, nullptr, rows, s));
       else TRY(run_tile_planes(ctx, (kind == 1 ? ctx->p_o : ctx->p_down)[l], kind == 1 ? D.d : act_frag(ctx, rows) ? 0 : D.Fpad, nullptr, rows, &launched, s));
     }

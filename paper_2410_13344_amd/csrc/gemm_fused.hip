@@ -154,14 +154,13 @@ __global__ __launch_bounds__(kWaves * 64) void k_qkv_rope(const FusedQkvArgs a) 
   const int d = D.d, dh = D.dh, half = dh / 2, spd = d / 16, sph = dh / 16;   // slabs per section / per head
   const int c = threadIdx.x & 15;
   const RowInfo ri = row_info(a.ssq, a.nb, d, D.eps, rows);
-  size_t cache_row[2];
-  int seq[2];
+  long long row_at[2];                                        // where the two rows go in the cache
   float2 rot[(NS + 1) / 2][2];                                // (cos, sin) of the two rows, per position pair
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int r = min(elem_row((int)threadIdx.x) + 32 * k, rows - 1);
-    seq[k] = a.rm.row_seq[r];
-    cache_row[k] = (size_t)(a.rm.seq_L[seq[k]] + a.rm.row_node[r]);
+    const int b = a.rm.row_seq[r];
+    row_at[k] = cache_row_at(a.cache, D, b, a.rm.seq_L[b] + a.rm.row_node[r], r);
 #pragma unroll
     for (int p = 0; p < (NS + 1) / 2; ++p) {
       const int s0 = slab[2 * p];
@@ -193,7 +192,6 @@ __global__ __launch_bounds__(kWaves * 64) void k_qkv_rope(const FusedQkvArgs a) 
       if (!ri.live[k]) continue;
       const int e = (int)threadIdx.x + 512 * k, r = elem_row(e);
       const float scale = ri.rs[k];
-      const int b = seq[k];
       if (section < 2) {
         // the pair is columns j and j + dh/2 of one head: rotate by pos * theta^(-2j/dh)
         const int h = (s0 % spd) / sph, j = (s0 % sph) * 16 + c;
@@ -205,8 +203,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_qkv_rope(const FusedQkvArgs a) 
           st_a(a.q + (size_t)r * d + c0, a.lo_off, y0);
           st_a(a.q + (size_t)r * d + c1, a.lo_off, y1);
         } else {
-          if (a.kv_layer) {   // (the benchmark hook has no cache to write to)
-            bf16_t* Kr = a.kv_layer + (((size_t)(0 * D.Bmax + b) * D.nH + h) * D.cap + cache_row[k]) * dh;
+          if (row_at[k] >= 0) {   // (the benchmark hook has no cache to write to)
+            bf16_t* Kr = (bf16_t*)a.cache.k + row_at[k] + h * a.cache.head_stride;
             Kr[j] = f32_to_bf16(y0);
             Kr[j + half] = f32_to_bf16(y1);
           }
@@ -220,8 +218,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_qkv_rope(const FusedQkvArgs a) 
           if (sv < 0) continue;
           const int col = (sv % spd) * 16 + c, h = col / dh, j = col % dh;
           const float y = pair_sum(red, which, e) * scale;
-          if (a.kv_layer) {
-            bf16_t* Vr = a.kv_layer + (((size_t)(1 * D.Bmax + b) * D.nH + h) * D.cap + cache_row[k]) * dh;
+          if (row_at[k] >= 0) {
+            bf16_t* Vr = (bf16_t*)a.cache.v + row_at[k] + h * a.cache.head_stride;
             Vr[j] = f32_to_bf16(y);
           }
           st_a(a.vtree + (size_t)r * d + col, a.lo_off, y);

@@ -43,7 +43,7 @@ hipError_t launch_assemble(const Dims& D, const TreeDev& tr, const RowMap& rm, c
                            const cerberus_taps& tp, int batch, int mode, const PromptArgs& pa, const AttnPlanCfg& ap, hipStream_t s);
 // rows of a step over pages, from what the plan of its rows left; lens [batch]: rows every sequence attends to
 hipError_t launch_assemble_pages(const Dims& D, const RowMap& rm, const cerberus_state& st, const cerberus_taps& tp, int batch,
-                                 const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s);
+                                 const cerberus_page_table& pt, const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s);
 // after the layers of a prompt pass: commits the rows; in the last pass the row map becomes that of the tail rows
 hipError_t launch_prompt_commit(const RowMap& rm, const cerberus_state& st, int* last_row, int batch, int seq, int last_pass,
                                 hipStream_t s);
@@ -61,8 +61,22 @@ enum { A_ROWS = 0, A_FRAG64 = 1, A_FRAG = 2 };
 int add_gain_blocks(int d, int order);   // sums per row
 hipError_t launch_add_gain(const Dims& D, const RowMap& rm, float* x, const float* part, int S, const int* S_dev, size_t pstride,
                            const float* gain, void* out, float* ssq, int rows_max, hipStream_t s, int order = A_ROWS);
+// Where a launch's new K/V rows go: the slab (row seq_L + node of the sequence), or, with slots, pages
+struct CacheRows {
+  void *k, *v;             // head 0's first row; null: nowhere
+  size_t head_stride;      // elements from a head's rows to the next one's
+  const int* slot;         // [rows] page * page_size + offset, below 0: no place; null: the slab
+  int page_shift;
+};
+// element of head 0 at which row r, row `row` of sequence b, begins; below 0: no place
+__device__ __forceinline__ long long cache_row_at(const CacheRows& c, const Dims& D, int b, int row, int r) {
+  if (!c.k) return -1;
+  if (!c.slot) return ((long long)b * D.nH * D.cap + row) * D.dh;
+  const int s = c.slot[r];
+  return s < 0 ? -1 : ((((long long)(s >> c.page_shift) * D.nH) << c.page_shift) + (s & ((1 << c.page_shift) - 1))) * D.dh;
+}
 hipError_t launch_rope_kv(const Dims& D, const RowMap& rm, const float* part, int S, size_t pstride,
-                          const float2* rope_cs, void* q, void* kv_layer, void* ktree, void* vtree, const float* ssq,
+                          const float2* rope_cs, void* q, const CacheRows& cache, void* ktree, void* vtree, const float* ssq,
                           int rows_max, hipStream_t s);
 // Whole-K GEMMs with fused epilogues (gemm_fused.hip), launches of up to 64 rows in bf16 mode.
 // At: the GEMM input in MFMA A-fragment order, piece [((ks * 2 + plane) * 4 + mt) * 64 + lane] = the 8 values
@@ -78,7 +92,7 @@ struct FusedQkvArgs {
   const float2* rope_cs;    // [rows][dh/2] (cos, sin) of every row's rotation angles (written by launch_embed)
   RowMap rm;
   bf16_t* q;                // [rows][d] hi, lo plane lo_off later
-  bf16_t* kv_layer;         // [2][Bmax][nH][cap][dh]
+  CacheRows cache;          // (launch_tile_qkv: the slab or nowhere)
   bf16_t* ktree;
   bf16_t* vtree;
   size_t lo_off;

@@ -216,13 +216,18 @@ hipError_t launch_assemble(const Dims& D, const TreeDev& tr, const RowMap& rm, c
 // out has a row nobody looks at (token 0, no slot, nothing to attend to, outside the taps).  slot: of the packed rows in, of the
 // sequences out.
 __global__ __launch_bounds__(64) void k_assemble_pages(const Dims D, const RowMap rm, const cerberus_state st, const cerberus_taps tp,
-                                                       int batch, const int* row_start, const int* first_pos, int* slot, int* lens) {
+                                                       int batch, const cerberus_page_table pt, const int* row_start, const int* first_pos,
+                                                       int* slot, int* lens) {
   const int b = threadIdx.x;
   bool runs = false;
   int own = -1;
   if (b < batch) {
     runs = first_pos[b] >= 0 && row_start[b + 1] > row_start[b];
     if (runs) own = slot[row_start[b]];
+    if (runs && (own < 0 || own / pt.page_size >= pt.n_pages)) {   // (a page number that no pool has)
+      atomicOr(pt.status, (int)CERBERUS_DEV_BAD_PAGE);
+      own = -1;
+    }
   }
   __syncthreads();                          // every packed slot has been read
   if (b == 0) *rm.n_rows = batch;
@@ -243,9 +248,9 @@ __global__ __launch_bounds__(64) void k_assemble_pages(const Dims D, const RowMa
 }
 
 hipError_t launch_assemble_pages(const Dims& D, const RowMap& rm, const cerberus_state& st, const cerberus_taps& tp, int batch,
-                                 const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s) {
+                                 const cerberus_page_table& pt, const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s) {
   static_assert(CERBERUS_MAX_BATCH <= 64, "a thread per sequence, one wave");
-  hipLaunchKernelGGL(k_assemble_pages, dim3(1), dim3(64), 0, s, D, rm, st, tp, batch, row_start, first_pos, slot, lens);
+  hipLaunchKernelGGL(k_assemble_pages, dim3(1), dim3(64), 0, s, D, rm, st, tp, batch, pt, row_start, first_pos, slot, lens);
   return hipGetLastError();
 }
 
@@ -541,7 +546,7 @@ __device__ __forceinline__ float row_rms_scale(const float* __restrict__ ssq, in
 // ---------------------------------------------------------------------------------------------
 template <typename T>
 __global__ void k_rope_kv(const float* __restrict__ part, int S, size_t pstride, const float2* __restrict__ rope_cs,
-                          const RowMap rm, T* __restrict__ q, size_t q_lo_off, T* __restrict__ kv_layer,
+                          const RowMap rm, T* __restrict__ q, size_t q_lo_off, const CacheRows cache,
                           T* __restrict__ ktree, T* __restrict__ vtree, const float* __restrict__ ssq, int nb, const Dims D) {
   const int r = blockIdx.x, h = blockIdx.y, j = threadIdx.x;
   if (r >= *rm.n_rows) return;
@@ -563,10 +568,10 @@ __global__ void k_rope_kv(const float* __restrict__ part, int S, size_t pstride,
   st_a(q + (size_t)r * d + c0, q_lo_off, v[0] * cs - v[1] * sn);
   st_a(q + (size_t)r * d + c1, q_lo_off, v[0] * sn + v[1] * cs);
   const float k0 = v[2] * cs - v[3] * sn, k1 = v[2] * sn + v[3] * cs;
-  const size_t row = (size_t)(rm.seq_L[b] + node);
-  if (kv_layer) {   // (a step over pages stores the rows itself)
-    T* Kr = kv_layer + (((size_t)(0 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
-    T* Vr = kv_layer + (((size_t)(1 * D.Bmax + b) * D.nH + h) * D.cap + row) * dh;
+  const long long row_at = cache_row_at(cache, D, b, rm.seq_L[b] + node, r);
+  if (row_at >= 0) {
+    T* Kr = (T*)cache.k + row_at + h * cache.head_stride;
+    T* Vr = (T*)cache.v + row_at + h * cache.head_stride;
     st_f(Kr + j, k0);
     st_f(Kr + j + half, k1);
     st_f(Vr + j, v[4]);
@@ -584,16 +589,16 @@ __global__ void k_rope_kv(const float* __restrict__ part, int S, size_t pstride,
 }
 
 hipError_t launch_rope_kv(const Dims& D, const RowMap& rm, const float* part, int S, size_t pstride,
-                          const float2* rope_cs, void* q, void* kv_layer, void* ktree, void* vtree, const float* ssq,
+                          const float2* rope_cs, void* q, const CacheRows& cache, void* ktree, void* vtree, const float* ssq,
                           int rows_max, hipStream_t s) {
   const int nb = add_gain_blocks(D.d, A_ROWS);
   dim3 grid(rows_max, D.nH), block(D.dh / 2);
   if (D.dtype == 0)
     hipLaunchKernelGGL((k_rope_kv<float>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (float*)q, (size_t)0,
-                       (float*)kv_layer, (float*)ktree, (float*)vtree, ssq, nb, D);
+                       cache, (float*)ktree, (float*)vtree, ssq, nb, D);
   else
     hipLaunchKernelGGL((k_rope_kv<bf16_t>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (bf16_t*)q,
-                       (size_t)D.R64 * D.d, (bf16_t*)kv_layer, (bf16_t*)ktree, (bf16_t*)vtree, ssq, nb, D);
+                       (size_t)D.R64 * D.d, cache, (bf16_t*)ktree, (bf16_t*)vtree, ssq, nb, D);
   return hipGetLastError();
 }
 

@@ -661,18 +661,19 @@ def _prompts(cfg, lens):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("page", [16, 64])
-def test_paged_step_equals_the_step_over_the_slab(dtype, page):
+@pytest.mark.parametrize("page,bounds,heads", [(16, True, {}), (64, False, {}), (32, False, dict(n_heads=2, head_dim=128)),
+                                              (16, True, dict(n_heads=2, head_dim=128))])
+def test_paged_step_equals_the_step_over_the_slab(dtype, page, bounds, heads):
     """The same prompts go on in the slab (ar_step) and in pages: logits, tokens, lengths, gate and the cache rows they add.
     Same sums but for the attention's order: the tiny shape's tolerance of the step against the oracle."""
-    pair = _pair(dtype)
+    pair = _pair(dtype, **heads)
     eng, cfg, lens, batch = pair.engine, pair.cfg, [37, 64, 5], 3
     tol = H.TOL_F32 if dtype == F32 else H.TOL_BF16_TINY
     st, sp = eng.new_state(), eng.new_state()
     for s in (st, sp):
         for b, p in enumerate(_prompts(cfg, lens)):
             eng.prefill(s, batch, b, p.to(torch.int32).cuda())
-    cache = B.PageCache(cfg["n_layers"], 40, page, cfg["n_heads"], cfg["head_dim"], dtype, 4, 8)
+    cache = B.PageCache(cfg["n_layers"], 40, page, cfg["n_heads"], cfg["head_dim"], dtype, 4, 8, bounds=bounds)
     eng.move_prompts(sp, cache, lens)
     assert cache.kv_len.tolist() == lens + [0]
     sp.kv.fill_(float("nan"))                               # the step over pages does not touch the slab
@@ -768,6 +769,56 @@ def test_paged_step_over_chosen_blocks(dtype):
     assert torch.isfinite(out[4]).all() and (out[4][2] - out[0][2]).abs().max() <= tol.logits    # three blocks of four
     assert not torch.equal(out[4][0], out[0][0])
     pair.engine.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_paged_step_in_a_captured_graph(dtype):
+    """Steps captured once and replayed, eager steps in between, against eager steps on another cache."""
+    pair = _pair(dtype)
+    eng, cfg, lens = pair.engine, pair.cfg, [100, 7, 40]
+    states = []
+    for _ in range(2):
+        sp = eng.new_state()
+        for b, p in enumerate(_prompts(cfg, lens)):
+            eng.prefill(sp, 3, b, p.to(torch.int32).cuda())
+        cache = B.PageCache(cfg["n_layers"], 60, 16, cfg["n_heads"], cfg["head_dim"], dtype, 3, 10)
+        eng.move_prompts(sp, cache, lens)
+        eng.paged_step(sp, cache, 3, n_select=5)
+        states.append((sp, cache))
+    (a, ca), (e, ce) = states
+    rows = torch.ones(3, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        eng.paged_step(a, ca, 3, rows, n_select=5)
+    for i in range(8):
+        rows.copy_(torch.tensor([1, i % 3 != 1, 1], dtype=torch.int32))
+        if i % 3 == 2:
+            eng.paged_step(a, ca, 3, rows)
+            eng.paged_step(e, ce, 3, rows)
+        graph.replay()
+        eng.paged_step(e, ce, 3, rows, n_select=5)
+        for n in ("root_token", "cand", "gate_flag", "entropy", "accept_len", "accepted_tokens", "status"):
+            assert torch.equal(getattr(a, n), getattr(e, n)), (i, n)
+        assert torch.equal(ca.words, ce.words) and torch.equal(ca.k, ce.k) and torch.equal(ca.v, ce.v) and torch.equal(ca.bounds, ce.bounds)
+    assert int(ca.status) == 0 and ca.kv_len.tolist() == [111, 15, 51]
+    pair.engine.close()
+
+
+def test_paged_step_without_a_page_number_of_the_pool():
+    """A free list that names no page of the pool: the row is written nowhere and the status says so."""
+    for bounds in (True, False):
+        pair = _pair(BF16)
+        eng, cfg = pair.engine, pair.cfg
+        sp = eng.new_state()
+        eng.prefill(sp, 1, 0, _prompts(cfg, [16])[0].to(torch.int32).cuda())
+        cache = B.PageCache(cfg["n_layers"], 4, 16, cfg["n_heads"], cfg["head_dim"], BF16, 1, 3, bounds=bounds)
+        eng.move_prompts(sp, cache, [16])
+        kept = cache.k.clone(), cache.v.clone()
+        cache.free_pages.fill_(5000)
+        eng.paged_step(sp, cache, 1)
+        assert int(cache.status) == B.CERBERUS_DEV_BAD_PAGE and torch.equal(cache.k, kept[0]) and torch.equal(cache.v, kept[1])
+        pair.engine.close()
 
 
 def test_generate_paged_equals_generate_without_the_tree():
