@@ -15,11 +15,7 @@ static_assert(kPlanThreads == CERBERUS_MAX_SEQS, "k_page_plan has a thread per s
 // inclusive sum over the workgroup's threads in order; sh holds an entry per wave and belongs to this sum alone
 __device__ __forceinline__ long long scan_sum(long long v, long long* sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const long long o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
+  v = wave_scan(v);
   if (lane == 63) sh[wave] = v;
   __syncthreads();
 #pragma unroll

@@ -71,6 +71,23 @@ struct PagedWorkspace {
 };
 PagedWorkspace paged_workspace(const cerberus_pages& pg, const cerberus_page_table& pt, int batch, int n_heads, int n_select, void* base);
 
+// Inclusive sum over the 64 lanes of a wave in order, all of them active.  Shifts within rows of 16 lanes, then the rows' last lanes handed on:
+// six adds without a trip through LDS (a scan by shuffles is ten times as long, and these kernels begin with it).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);    // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return v;
+}
+// the same for sums past 32 bits, of terms in 0 .. 2^40
+__device__ __forceinline__ long long wave_scan(long long v) {
+  const int lo = wave_scan((int)(v & 0xfffff)), hi = wave_scan((int)(v >> 20));
+  return ((long long)hi << 20) + lo;
+}
+
 // argument checks of the public entry points, also those of the step over pages
 int check_pages(const cerberus_pages* pg);
 int check_page_table(const cerberus_page_table* pt, int batch);

@@ -34,8 +34,10 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
   const int lane = threadIdx.x & 63, k = (a.batch + 63) >> 6, b0 = lane * k, b1 = min(a.batch, b0 + k);
   long long total = 0;
   for (int b = b0; b < b1; ++b) total += rows_of(a, b);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
+  {
+    const int lo = __builtin_amdgcn_readlane(wave_scan((int)(total & 0xfffff)), 63), hi = __builtin_amdgcn_readlane(wave_scan((int)(total >> 20)), 63);
+    total = ((long long)hi << 20) + lo;
+  }
   Cut c;
   // as many pieces as the launch has workgroups for (at most per_head + one per sequence), half as many where they would be short
   const long long full = (total + per_head - 1) / per_head, half = (total + (per_head + 1) / 2 - 1) / ((per_head + 1) / 2);
@@ -48,18 +50,13 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
     n += p;
     cuts += p > 1 ? p : 0;
   }
-  int n_end = n, cut_end = cuts;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int x = __shfl_up(n_end, off, 64), y = __shfl_up(cut_end, off, 64);
-    if (lane >= off) { n_end += x; cut_end += y; }
-  }
+  const int both = wave_scan(n | cuts << 16), n_end = both & 0xffff, cut_end = both >> 16;   // (each at most 2 * CERBERUS_MAX_SEQS)
   const unsigned long long mine = __ballot(of_seq ? item >= b0 && item < b1 : item >= n_end - n && item < n_end);
   c.b = -1;
   c.j = c.pieces = c.slot0 = 0;
   if (mine == 0) return c;
   const int owner = __ffsll((long long)mine) - 1;
-  int at = __shfl(n_end - n, owner, 64), slot = __shfl(cut_end - cuts, owner, 64);
+  int at = __builtin_amdgcn_readlane(n_end - n, owner), slot = __builtin_amdgcn_readlane(cut_end - cuts, owner);
   for (int b = owner * k; b < a.batch; ++b) {
     const int p = pieces_of(b);
     if (of_seq ? b == item : item < at + p) {
