@@ -271,12 +271,13 @@ int cerberus_paged_attention(const cerberus_pages *pg, const cerberus_page_table
                              void *out, int64_t out_row_stride, int32_t batch, int32_t n_heads, float scale,
                              const int32_t *blocks, int32_t n_select, void *workspace, size_t workspace_bytes, void *stream);
 
-/* cerberus_ar_step with the cache in pages: layers (HOST [n_layers]) are the pages of every layer (all of one shape: the model's heads, its
- * head_dim and dtype).  new_rows (DEVICE [batch], NULL: 1 for all): 1 the sequence decodes a token, 0 it sits the step
- * out, below 0 it ends.  A sequence without room for its row sits out too (CERBERUS_DEV_KV_OVERFLOW in pt->status).
- * n_select > 0: every layer attends to that many blocks, chosen per layer (needs bounds).  st as in cerberus_ar_step, but
- * st->kv and st->kv_len are not used; the rows are counted in pt->kv_len.  In bf16 mode the token's own row is attended to as
- * the cache holds it, in bf16.                                                                  */
+/* cerberus_ar_step with the cache in pages: layers (HOST [n_layers]) are the pages of every layer, all of one shape: the model's
+ * heads, its head_dim and dtype.  new_rows (DEVICE [batch], NULL: 1 for all): 1 the sequence decodes a token, 0 it sits the
+ * step out, below 0 it ends.  A sequence without room for its row sits out too (CERBERUS_DEV_KV_OVERFLOW in pt->status).
+ * n_select > 0: every layer attends to that many blocks, chosen per layer and head (needs bounds).  st as in
+ * cerberus_ar_step, but st->kv and st->kv_len are not used: the rows are counted in pt->kv_len.  The new row's K and V are
+ * attended to at the precision of the computation, as in cerberus_ar_step; the pages keep them in their type, and their bounds
+ * if they have any.  max_batch of the context bounds the batch, kv_capacity does not matter.                          */
 int cerberus_paged_step(cerberus_ctx *ctx, const cerberus_state *st, const cerberus_pages *layers, const cerberus_page_table *pt,
                         int32_t batch, const int32_t *new_rows, int32_t n_select, void *workspace, size_t workspace_bytes,
                         void *stream);

@@ -402,6 +402,8 @@ class PageCache:
 
     def _on(self, stream):
         """Makes the cache's device and the call's stream torch's current ones."""
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device} for a cache on {self.device}")
         return torch.cuda.stream(torch.cuda.current_stream(self.device) if stream is None else stream)
 
     def _stream(self) -> int:

@@ -623,6 +623,25 @@ def test_calls_in_a_captured_graph_and_on_another_stream():
     assert int(a.status) == 0
 
 
+def test_calls_on_two_streams_at_once():
+    """Workspaces and outputs come per call and stream: cut attention and long choices side by side give what they give alone."""
+    caches = [filled(BF16, 8, 2, 64, 16, lens, seed=i, poison=False) for i, lens in enumerate(([20000, 300], [18000, 7]))]
+    for c, *_ in caches:
+        c.bounds.normal_()
+    qs = [x[4].cuda() for x in caches]
+    alone = [(c.attention(0, q), c.select(0, q, 100)) for (c, *_), q in zip(caches, qs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            got[i].append((caches[i][0].attention(0, qs[i], stream=s), caches[i][0].select(0, qs[i], 100, stream=s)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for x, y in got[i]:
+            assert torch.equal(x, alone[i][0]) and torch.equal(y, alone[i][1])
+
+
 def test_refusals_of_the_binding():
     c = B.PageCache(1, 8, 16, 2, 64, BF16, 3, 4)
     q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
