@@ -56,7 +56,7 @@ struct PagedAttnArgs {
   float* part;                              // workspace
   int* status;
 };
-size_t paged_attention_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int max_blocks, int page_size, int n_select);
+size_t paged_attention_bytes(int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, hipStream_t s);
 
 // What lies where in the workspace of the calls over pages

@@ -66,7 +66,7 @@ PagedWorkspace paged_workspace(const cerberus_pages& pg, const cerberus_page_tab
   };
   const size_t row = (size_t)batch * pg.n_kv_heads;
   PagedWorkspace w{};
-  w.part = reinterpret_cast<float*>(take(paged_attention_bytes(batch, n_heads, pg.n_kv_heads, pg.head_dim, pt.max_blocks, pt.page_size, n_select)));
+  w.part = reinterpret_cast<float*>(take(paged_attention_bytes(n_heads, pg.n_kv_heads, pg.head_dim)));
   w.keys = reinterpret_cast<unsigned long long*>(take(n_select ? page_select_bytes(batch, pg.n_kv_heads, pt.max_blocks) : 0));
   w.row_start = reinterpret_cast<int*>(take((size_t)(batch + 1) * 4));
   w.first_pos = reinterpret_cast<int*>(take((size_t)batch * 4));

@@ -11,8 +11,6 @@ namespace {
 
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 
-constexpr int kShort = 512;      // rows below which a piece's beginning and end show in its time
-
 // How the rows of a batch are cut.  Sequence b has rows_of(b) rows to look at (with chosen blocks: the rows of all places of
 // its list); they are cut into pieces of `piece` rows, a multiple of what a workgroup takes at a time, and every (piece, key
 // head, 16 of its query heads) is a workgroup.  A sequence of one piece is written out by its workgroup, the pieces of
@@ -29,7 +27,20 @@ __device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int b) {
   return a.blocks && L > 0 ? a.n_select << a.page_shift : L;
 }
 
-// unit: pieces are a multiple of so many rows.  item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks after sequences l * k .. l * k + k - 1.
+// Rows of a piece if there are `total` and per_head pieces are wanted, which makes eight workgroups for every compute unit, where two run
+// at a time: many pieces even out sequences of all lengths, but a piece's beginning and end show in its time.
+// So pieces are not cut below 1024 rows for the last half of them, nor below 512 for the third quarter.  us with per_head pieces for
+// 512 / 1024 / 2048 workgroups without those two limits: 64 sequences of up to 16384 rows x 8 key heads 204 / 192 / 184, one of 131072 91 / 90 / 96,
+// 16 of 257..2049 rows x 32 heads 66 / 63 / 62, lists of 2048 rows for 16 x 8 key heads 31 / 35 / 37.
+__host__ __device__ __forceinline__ long long piece_rows(long long total, int per_head) {
+  const int half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
+  const long long a = (total + per_head - 1) / per_head, b = (total + half - 1) / half, c = (total + quarter - 1) / quarter;
+  const long long b1 = b < 1024 ? b : 1024, c1 = c < 512 ? c : 512;
+  return a > b1 ? (a > c1 ? a : c1) : (b1 > c1 ? b1 : c1);
+}
+
+// unit: pieces are a multiple of so many rows.  item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks
+// after sequences l * k .. l * k + k - 1.
 __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
   const int lane = threadIdx.x & 63, k = (a.batch + 63) >> 6, b0 = lane * k, b1 = min(a.batch, b0 + k);
   long long total = 0;
@@ -39,9 +50,7 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
     total = ((long long)hi << 20) + lo;
   }
   Cut c;
-  // as many pieces as the launch has workgroups for (at most per_head + one per sequence), half as many where they would be short
-  const long long full = (total + per_head - 1) / per_head, half = (total + (per_head + 1) / 2 - 1) / ((per_head + 1) / 2);
-  const long long want = max(full, min(half, (long long)kShort));
+  const long long want = piece_rows(total, per_head);
   c.piece = (int)min((max(want, 1ll) + unit - 1) / unit * unit, (long long)INT_MAX);   // (at INT_MAX nothing is cut)
   auto pieces_of = [&](int b) { return max(1, (int)(((unsigned)rows_of(a, b) + (unsigned)c.piece - 1u) / (unsigned)c.piece)); };
   int n = 0, cuts = 0;
@@ -50,7 +59,7 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
     n += p;
     cuts += p > 1 ? p : 0;
   }
-  const int both = wave_scan(n | cuts << 16), n_end = both & 0xffff, cut_end = both >> 16;   // (each at most 2 * CERBERUS_MAX_SEQS)
+  const int both = wave_scan(n | cuts << 16), n_end = both & 0xffff, cut_end = both >> 16;   // (items: a piece per sequence and kTarget, cut ones: 2 kTarget at most)
   const unsigned long long mine = __ballot(of_seq ? item >= b0 && item < b1 : item >= n_end - n && item < n_end);
   c.b = -1;
   c.j = c.pieces = c.slot0 = 0;
@@ -106,6 +115,10 @@ template <int DH> struct Stage<float, DH> {
 //                 fp32: product (r, c, i) contracts keys 4 g + i over g and gives columns 64 r + 4 n + c.
 // A lane's outputs all belong to its query, so the running maximum's factor is the lane's own.
 // bf16: probabilities go into the second product as two bf16 planes (p to 2^-17): the matrix units have time.
+// Two waves per SIMD with 256 registers each: 16 KB of K and V in work and 16 KB in flight per wave, 128 KB in flight per compute unit.
+// Measured (bf16, 128 columns, this kernel alone): 131072 rows x 8 key heads 81-92 us, 5.8-6.6 TB/s with the matrix units busy 6 % of the time; 64
+// sequences of up to 16384 rows x 8 key heads 180, 6.1; 16 of 257..2049 x 32 heads 54, 6.0; 1025 rows x 32 heads 6.6, which
+// is the chain of length, table, rows and join.  A copy of 1 GiB runs at 5.1 TB/s.
 // STEP: a decoding step's queries and outputs are two bf16 planes, and the newest row has a second plane next to the cache.
 // ---------------------------------------------------------------------------------------------
 // ONCE: K and V are read once in the launch (up to 16 queries per key head): loaded with the streaming hint.  A model's layers hold more
@@ -406,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, in
 }
 
 // Joins the pieces of a sequence: a workgroup takes `heads` (a power of two) heads, groups of DH / 4 lanes take pieces in turn,
-// four at a time.
+// four at a time.  3.4 to 4.5 us, the chain of lengths, partial results and LDS; a head per workgroup 6.2 for 64 sequences x 32 heads.
 template <typename T, int DH, bool STEP>
 __global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int unit, int per_head, int heads) {
   constexpr int LPP = DH / 4, GROUPS = 256 / LPP;
@@ -468,23 +481,31 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int u
 
 namespace {
 
-constexpr int kTarget = 1024;     // workgroups a launch aims for, four per compute unit (two run at a time)
-constexpr int kWhole = 512;       // rows that one workgroup reads in less time than a join takes
-constexpr int kLists = 256;       // workgroups that keep the memory busy
+constexpr int kTarget = 2048;     // workgroups a launch aims for at most
+constexpr int kTurns = 4;         // turns of a workgroup that take less time than a join
+constexpr int kLists = 256;       // workgroups that keep the memory busy: 128 lists of 2048 rows take 38.3 us whole, 31.8 cut and joined
 
 int head_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 // pieces that a launch aims for per (key head, 16 queries)
 int per_head_of(int n_heads, int n_kv_heads) { return std::max(1, kTarget / (n_kv_heads * head_tiles(n_heads, n_kv_heads))); }
 
+// total / piece_rows(total) is no more than this for any total up to `rows`: each of the three limits of piece_rows bounds it
+long long pieces_at_most(long long rows, int per_head) {
+  const long long half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
+  return std::min<long long>({per_head, std::max(half, (rows + 1023) / 1024), std::max(quarter, (rows + 511) / 512)});
+}
+
 template <typename T, int DH, bool STEP>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
   const int tiles = head_tiles(a.n_heads, a.pg.n_kv_heads), per_head = per_head_of(a.n_heads, a.pg.n_kv_heads);
-  // Joining pieces is a launch of its own, 5 to 8 us with what goes before it, and a workgroup by itself reads about 90 rows a us
-  // (bf16, 128 columns).  So nothing is cut where all that the table or the list has room for is kWhole rows, and lists, which
-  // are of one length, are not where they are enough workgroups to keep the memory busy.
-  const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift;
-  const bool cuts = most > kWhole && !(a.blocks && (long long)a.batch * a.pg.n_kv_heads * tiles >= kLists);
-  const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512, items = (int)std::min<long long>(a.batch + per_head, a.batch * ((most - 1) / unit + 1));
+  // Joining pieces is a launch of its own, 5 to 8 us with what goes before it, and a workgroup by itself takes about 1.4 us a turn.  So
+  // nothing is cut where all that the table or the list has room for is a few turns, twice as many where every compute unit has
+  // its two workgroups anyway (us, 32 heads, cut / whole: 256 rows 10.3 / 7.7, 500 10.4 / 10.6, 1000 11.1 / 18.0; 16 sequences of 1000 50.1 / 45.4),
+  // and lists, which are of one length, are not where they are enough workgroups to keep the memory busy.
+  const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift, pairs = (long long)a.batch * a.pg.n_kv_heads * tiles;
+  const bool cuts = most > kTurns * kUnit<T> * (pairs >= 512 ? 2 : 1) && !(a.blocks && pairs >= kLists);
+  const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512;
+  const int items = (int)std::min(a.batch + pieces_at_most(a.batch * most, per_head), a.batch * ((most - 1) / unit + 1));
   const long long all = ((long long)items * a.pg.n_kv_heads + 7) / 8 * 8 * tiles, row = std::max(8ll * tiles, (1ll << 18) / (8 * tiles) * (8 * tiles));
   const dim3 grid((unsigned)std::min(all, row), (unsigned)((all - 1) / row + 1));
   if (STEP || tiles == 1) hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, true>), grid, dim3(256), 0, s, a, unit, per_head, tiles, items);   // (a step's heads share no keys)
@@ -500,7 +521,7 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 // partial results: cut sequences have at most 2 per_head pieces (see find_cut: a cut one has more than `piece` rows)
-size_t paged_attention_bytes(int batch, int n_heads, int n_kv_heads, int head_dim, int max_blocks, int page_size, int n_select) {
+size_t paged_attention_bytes(int n_heads, int n_kv_heads, int head_dim) {
   return (size_t)2 * per_head_of(n_heads, n_kv_heads) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
