@@ -201,7 +201,8 @@ int cerberus_accept_noalloc(cerberus_ctx *ctx, const int32_t *node_argmax, const
  * A key-value cache in pages.  The slab of cerberus_state reserves kv_capacity rows for every sequence; here sequences
  * share a pool of pages and hold as many as their length needs.  A page is page_size rows (a power of two, 16..256) of every
  * key head; row r of a sequence lies in block r / page_size of its block table, at offset r % page_size of that page.  The calls
- * below need no context; they run on the device that is current, allocate nothing and may be captured into a graph.
+ * below need no context; they run on the device that is current, allocate nothing and may be captured into a graph.  A page
+ * belongs to one sequence: tables that share pages are read as they stand, but would hand such a page back twice.
  * One layer's pages and the tables (which all layers share):                                     */
 typedef struct {
   void *k, *v;            /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned     */

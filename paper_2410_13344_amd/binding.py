@@ -236,12 +236,14 @@ def cerberus_accept_noalloc(ctx: int, node_argmax: torch.Tensor, node_token: tor
 
 def cerberus_page_plan(table: PageTable, new_rows: torch.Tensor, max_rows: int, row_start: torch.Tensor, first_pos: torch.Tensor,
                        slot: torch.Tensor, stream=None) -> None:
+    assert all(t.is_cuda and t.dtype == torch.int32 for t in (new_rows, row_start, first_pos, slot))
     _check(lib().cerberus_page_plan(table, new_rows.data_ptr(), new_rows.shape[0], max_rows, row_start.data_ptr(),
                                     first_pos.data_ptr(), slot.data_ptr(), _stream_ptr(stream)))
 
 
 def cerberus_page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, status: Optional[torch.Tensor] = None,
                         stream=None) -> None:
+    assert k.is_cuda and v.is_cuda and slot.is_cuda and slot.dtype == torch.int32 and k.shape == v.shape and k.shape[0] == slot.shape[0]
     _check(lib().cerberus_page_store(pages, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                                      slot.data_ptr(), slot.shape[0], _ptr(status), _stream_ptr(stream)))
 
@@ -252,12 +254,14 @@ def cerberus_paged_workspace_bytes(pages: Pages, table: PageTable, batch: int, n
 
 def cerberus_page_select(pages: Pages, table: PageTable, q: torch.Tensor, blocks: torch.Tensor, workspace: torch.Tensor,
                          stream=None) -> None:
+    assert q.is_cuda and workspace.is_cuda and blocks.is_cuda and blocks.dtype == torch.int32 and blocks.shape[0] == q.shape[0]
     _check(lib().cerberus_page_select(pages, table, q.data_ptr(), q.stride(0), q.shape[0], q.shape[1], blocks.shape[2],
                                       blocks.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
 
 
 def cerberus_paged_attention(pages: Pages, table: PageTable, q: torch.Tensor, out: torch.Tensor, scale: float,
                              blocks: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    assert q.is_cuda and out.is_cuda and workspace.is_cuda and out.shape == q.shape and (blocks is None or blocks.is_cuda)
     _check(lib().cerberus_paged_attention(pages, table, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), q.shape[0], q.shape[1],
                                           scale, _ptr(blocks), 0 if blocks is None else blocks.shape[2], workspace.data_ptr(),
                                           workspace.numel(), _stream_ptr(stream)))
@@ -265,6 +269,7 @@ def cerberus_paged_attention(pages: Pages, table: PageTable, q: torch.Tensor, ou
 
 def cerberus_paged_step(ctx: int, state: State, layers, table: PageTable, batch: int, new_rows: Optional[torch.Tensor], n_select: int,
                         workspace: torch.Tensor, stream=None) -> None:
+    assert workspace.is_cuda and (new_rows is None or (new_rows.is_cuda and new_rows.dtype == torch.int32))
     _check(lib().cerberus_paged_step(ctx, C.byref(state), layers, table, batch, _ptr(new_rows), n_select, workspace.data_ptr(),
                                      workspace.numel(), _stream_ptr(stream)))
 
@@ -356,6 +361,10 @@ class PageCache:
             raise ValueError("non-positive size of a page cache")
         self.dtype = torch.float32 if dtype == CERBERUS_F32 else torch.bfloat16
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("a page cache lives on a HIP device")
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU: the Cerberus library only runs on a HIP device")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         device, self._index = self.device, self.device.index

@@ -32,7 +32,7 @@ __device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int b) {
 // So pieces are not cut below 1024 rows for the last half of them, nor below 512 for the third quarter.  us with per_head pieces for
 // 512 / 1024 / 2048 workgroups without those two limits: 64 sequences of up to 16384 rows x 8 key heads 204 / 192 / 184, one of 131072 91 / 90 / 96,
 // 16 of 257..2049 rows x 32 heads 66 / 63 / 62, lists of 2048 rows for 16 x 8 key heads 31 / 35 / 37.
-__host__ __device__ __forceinline__ long long piece_rows(long long total, int per_head) {
+__device__ __forceinline__ long long piece_rows(long long total, int per_head) {
   const int half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
   const long long a = (total + per_head - 1) / per_head, b = (total + half - 1) / half, c = (total + quarter - 1) / quarter;
   const long long b1 = b < 1024 ? b : 1024, c1 = c < 512 ? c : 512;
@@ -479,6 +479,14 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int u
   }
 }
 
+// Pieces of a batch at most, its sequences being no longer than `most` rows: one for each and one for every piece_rows(total) rows, and
+// each of the three limits of piece_rows bounds the number of those for any total.
+int paged_attention_items(int batch, long long most, int unit, int per_head) {
+  const long long rows = batch * most, half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
+  const long long cuts = std::min<long long>({per_head, std::max(half, (rows + 1023) / 1024), std::max(quarter, (rows + 511) / 512)});
+  return (int)std::min(batch + cuts, batch * ((most - 1) / unit + 1));
+}
+
 namespace {
 
 constexpr int kTarget = 2048;     // workgroups a launch aims for at most
@@ -488,12 +496,6 @@ constexpr int kLists = 256;       // workgroups that keep the memory busy: 128 l
 int head_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 // pieces that a launch aims for per (key head, 16 queries)
 int per_head_of(int n_heads, int n_kv_heads) { return std::max(1, kTarget / (n_kv_heads * head_tiles(n_heads, n_kv_heads))); }
-
-// total / piece_rows(total) is no more than this for any total up to `rows`: each of the three limits of piece_rows bounds it
-long long pieces_at_most(long long rows, int per_head) {
-  const long long half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
-  return std::min<long long>({per_head, std::max(half, (rows + 1023) / 1024), std::max(quarter, (rows + 511) / 512)});
-}
 
 template <typename T, int DH, bool STEP>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
@@ -505,7 +507,7 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
   const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift, pairs = (long long)a.batch * a.pg.n_kv_heads * tiles;
   const bool cuts = most > kTurns * kUnit<T> * (pairs >= 512 ? 2 : 1) && !(a.blocks && pairs >= kLists);
   const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512;
-  const int items = (int)std::min(a.batch + pieces_at_most(a.batch * most, per_head), a.batch * ((most - 1) / unit + 1));
+  const int items = paged_attention_items(a.batch, most, unit, per_head);
   const long long all = ((long long)items * a.pg.n_kv_heads + 7) / 8 * 8 * tiles, row = std::max(8ll * tiles, (1ll << 18) / (8 * tiles) * (8 * tiles));
   const dim3 grid((unsigned)std::min(all, row), (unsigned)((all - 1) / row + 1));
   if (STEP || tiles == 1) hipLaunchKernelGGL((k_paged_attn<T, DH, STEP, true>), grid, dim3(256), 0, s, a, unit, per_head, tiles, items);   // (a step's heads share no keys)

@@ -665,6 +665,8 @@ def test_refusals_of_the_binding():
         B.PageCache(1, 8, 16, 2, 64, 7, 3, 4)
     with pytest.raises(ValueError):
         B.PageCache(1, 0, 16, 2, 64, BF16, 3, 4)
+    with pytest.raises(ValueError):
+        B.PageCache(1, 8, 16, 2, 64, BF16, 3, 4, device="cpu")
 
 
 # ------------------------------------------------------------------------------------------------

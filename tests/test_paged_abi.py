@@ -137,6 +137,11 @@ def test_step_arguments_without_a_context(L):
     assert L.cerberus_paged_step(None, C.byref(st), pg, pt, 1, None, 0, A, 1 << 30, None) == ARG
 
 
+def test_a_page_cache_needs_a_gpu():
+    with pytest.raises(ValueError):
+        B.PageCache(1, 8, 16, 2, 64, B.CERBERUS_BF16, 3, 4, device="cpu")
+
+
 def test_constants_match_the_header():
     text = open(os.path.join(os.path.dirname(B.LIB_PATH), "..", "include", "cerberus.h")).read()
     for name, value in (("CERBERUS_DEV_BAD_PAGE", B.CERBERUS_DEV_BAD_PAGE), ("CERBERUS_MAX_SEQS", B.CERBERUS_MAX_SEQS)):
