@@ -725,6 +725,35 @@ def test_paged_step_equals_the_step_over_the_slab(dtype, page, bounds, heads):
     pair.engine.close()
 
 
+@pytest.mark.parametrize("bounds", [True, False])
+def test_paged_step_at_full_width(bounds):
+    """The 7B shape's width and heads, two layers: the projection kernels that the small shape does not reach, 16 sequences of mixed
+    lengths.  The bar of a step's logits against the oracle."""
+    cfg = synth.make_config("7b", n_layers=2, vocab=1024, n_resblocks=1, special_block=-1)
+    W = synth.make_weights(cfg, seed=1, dtype=torch.bfloat16, device="cuda")
+    parent, rank = synth.make_tree("tiny", 4)
+    eng = B.Engine(cfg, W, parent, rank, BF16, max_batch=16, kv_capacity=700)
+    lens = [1 + 43 * b for b in range(16)]
+    st = eng.new_state()
+    for b, p in enumerate(_prompts(cfg, lens)):
+        eng.prefill(st, 16, b, p.to(torch.int32).cuda())
+    cache = B.PageCache(2, 600, 16, 32, 128, BF16, 16, 50, bounds=bounds)
+    eng.move_prompts(st, cache, lens)
+    taps = B.DeviceTaps(cfg, 16, len(parent))
+    eng.set_taps(taps)
+    rows = torch.arange(16, device="cuda") * len(parent)
+    for _ in range(2):
+        roots = st.root_token.clone()
+        eng.paged_step(st, cache, 16)
+        got, tokens = taps.logits[rows].clone(), st.accepted_tokens[:, 0].clone()
+        st.root_token.copy_(roots)
+        eng.ar_step(st, 16)
+        assert (got - taps.logits[rows]).abs().max() <= H.TOL_BF16.logits and torch.equal(tokens, st.accepted_tokens[:, 0])
+        assert torch.equal(cache.kv_len, st.kv_len)
+    assert int(cache.status) == 0 and int(st.status) == 0
+    eng.close()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_paged_step_sits_out_ends_and_runs_out_of_pages(dtype):
     pair = _pair(dtype)
