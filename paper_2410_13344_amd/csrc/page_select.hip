@@ -306,7 +306,10 @@ void launch(const PageSelectArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_page_choose<T, DH>), dim3(a.pg.n_kv_heads, a.batch), dim3(kChooseThreads), 0, s, a);
     return;
   }
-  const int once = 4 * Scores<T, DH>::AT_ONCE, along = (int)std::min<long long>(((long long)a.max_blocks + once - 1) / once, 4096);
+  // (A wide table's sequences may be short: no more workgroups than keep the memory busy if every list is long.  64 sequences of 32 blocks with
+  // room for 8192 took 64 us with a workgroup for every part of the table.)
+  const int once = 4 * Scores<T, DH>::AT_ONCE, lists = a.pg.n_kv_heads * a.batch;
+  const int along = (int)std::min<long long>(((long long)a.max_blocks + once - 1) / once, std::max(1, 2048 / lists));
   hipLaunchKernelGGL((k_page_scores<T, DH>), dim3(along, a.pg.n_kv_heads, a.batch), dim3(256), 0, s, a);
   hipLaunchKernelGGL(k_page_pick, dim3(a.pg.n_kv_heads, a.batch), dim3(1024), 0, s, a);
 }

@@ -56,7 +56,7 @@ struct PagedAttnArgs {
   float* part;                              // workspace
   int* status;
 };
-int paged_attention_items(int batch, long long most, int unit, int per_head);   // pieces that a launch has workgroups for
+int paged_attention_items(int batch, long long most, int unit, int per_head);   // pieces that a launch has workgroups for (unit 0: nothing is cut)
 size_t paged_attention_bytes(int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, hipStream_t s);
 

@@ -39,12 +39,17 @@ __device__ __forceinline__ long long piece_rows(long long total, int per_head) {
   return a > b1 ? (a > c1 ? a : c1) : (b1 > c1 ? b1 : c1);
 }
 
-// unit: pieces are a multiple of so many rows.  item: which one to find, or (of_seq) the first one of that sequence.  Lane l looks
-// after sequences l * k .. l * k + k - 1.
-__device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
-  const int lane = threadIdx.x & 63, k = (a.batch + 63) >> 6, b0 = lane * k, b1 = min(a.batch, b0 + k);
+// unit: pieces are a multiple of so many rows; 0: nothing is cut.  item: which one to find, or (of_seq) the first one of that sequence.
+// Lane l looks after sequences l, l + 64, .. (K of them at most); pieces are counted lane by lane.
+template <int K>
+__device__ __forceinline__ Cut find_cut_of(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
+  const int lane = threadIdx.x & 63, k = K == 1 ? 1 : (a.batch + 63) >> 6;
+  int rows[K];                                                      // (all loads in flight before the first sum)
+#pragma unroll
+  for (int i = 0; i < K; ++i) rows[i] = i < k && i * 64 + lane < a.batch ? rows_of(a, i * 64 + lane) : 0;
   long long total = 0;
-  for (int b = b0; b < b1; ++b) total += rows_of(a, b);
+#pragma unroll
+  for (int i = 0; i < K; ++i) total += rows[i];
   {
     const int lo = __builtin_amdgcn_readlane(wave_scan((int)(total & 0xfffff)), 63), hi = __builtin_amdgcn_readlane(wave_scan((int)(total >> 20)), 63);
     total = ((long long)hi << 20) + lo;
@@ -52,30 +57,35 @@ __device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool o
   Cut c;
   const long long want = piece_rows(total, per_head);
   c.piece = (int)min((max(want, 1ll) + unit - 1) / unit * unit, (long long)INT_MAX);   // (at INT_MAX nothing is cut)
-  auto pieces_of = [&](int b) { return max(1, (int)(((unsigned)rows_of(a, b) + (unsigned)c.piece - 1u) / (unsigned)c.piece)); };
+  const unsigned piece = c.piece;
   int n = 0, cuts = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int p = pieces_of(b);
-    n += p;
-    cuts += p > 1 ? p : 0;
-  }
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+    if (i < k) {                                                    // rows[i] becomes the sequence's pieces
+      rows[i] = i * 64 + lane < a.batch ? max(1, (int)(((unsigned)rows[i] + piece - 1u) / piece)) : 0;
+      n += rows[i];
+      cuts += rows[i] > 1 ? rows[i] : 0;
+    }
   const int both = wave_scan(n | cuts << 16), n_end = both & 0xffff, cut_end = both >> 16;   // (items: a piece per sequence and kTarget, cut ones: 2 kTarget at most)
-  const unsigned long long mine = __ballot(of_seq ? item >= b0 && item < b1 : item >= n_end - n && item < n_end);
+  const unsigned long long mine = __ballot(of_seq ? item % 64 == lane : item >= n_end - n && item < n_end);
   c.b = -1;
   c.j = c.pieces = c.slot0 = 0;
   if (mine == 0) return c;
   const int owner = __ffsll((long long)mine) - 1;
   int at = __builtin_amdgcn_readlane(n_end - n, owner), slot = __builtin_amdgcn_readlane(cut_end - cuts, owner);
-  for (int b = owner * k; b < a.batch; ++b) {
-    const int p = pieces_of(b);
-    if (of_seq ? b == item : item < at + p) {
-      c.b = b; c.j = of_seq ? 0 : item - at; c.pieces = p; c.slot0 = slot;
-      break;
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+    if (i < k) {
+      const int b = i * 64 + owner, p = __builtin_amdgcn_readlane(rows[i], owner);
+      if (c.b < 0 && (of_seq ? b == item : item < at + p)) { c.b = b; c.j = of_seq ? 0 : item - at; c.pieces = p; c.slot0 = slot; }
+      at += p;
+      slot += p > 1 ? p : 0;
     }
-    at += p;
-    slot += p > 1 ? p : 0;
-  }
   return c;
+}
+__device__ __forceinline__ Cut find_cut(const PagedAttnArgs& a, int item, bool of_seq, int unit, int per_head) {
+  if (unit == 0) return Cut{INT_MAX, item, 0, 1, 0};
+  return a.batch <= 64 ? find_cut_of<1>(a, item, of_seq, unit, per_head) : find_cut_of<CERBERUS_MAX_SEQS / 64>(a, item, of_seq, unit, per_head);
 }
 
 template <typename T> struct Tile;      // 16-key tiles a wave takes at a time
@@ -482,6 +492,7 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedAttnArgs a, int u
 // Pieces of a batch at most, its sequences being no longer than `most` rows: one for each and one for every piece_rows(total) rows, and
 // each of the three limits of piece_rows bounds the number of those for any total.
 int paged_attention_items(int batch, long long most, int unit, int per_head) {
+  if (unit == 0) return batch;
   const long long rows = batch * most, half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
   const long long cuts = std::min<long long>({per_head, std::max(half, (rows + 1023) / 1024), std::max(quarter, (rows + 511) / 512)});
   return (int)std::min(batch + cuts, batch * ((most - 1) / unit + 1));
@@ -506,7 +517,7 @@ void launch(const PagedAttnArgs& a, hipStream_t s) {
   // and lists, which are of one length, are not where they are enough workgroups to keep the memory busy.
   const long long most = (long long)(a.blocks ? a.n_select : a.max_blocks) << a.page_shift, pairs = (long long)a.batch * a.pg.n_kv_heads * tiles;
   const bool cuts = most > kTurns * kUnit<T> * (pairs >= 512 ? 2 : 1) && !(a.blocks && pairs >= kLists);
-  const int unit = cuts ? kUnit<T> : INT_MAX / 512 * 512;
+  const int unit = cuts ? kUnit<T> : 0;
   const int items = paged_attention_items(a.batch, most, unit, per_head);
   const long long all = ((long long)items * a.pg.n_kv_heads + 7) / 8 * 8 * tiles, row = std::max(8ll * tiles, (1ll << 18) / (8 * tiles) * (8 * tiles));
   const dim3 grid((unsigned)std::min(all, row), (unsigned)((all - 1) / row + 1));
