@@ -277,8 +277,8 @@ int cerberus_paged_attention(const cerberus_pages *pg, const cerberus_page_table
  * step out, below 0 it ends.  A sequence without room for its row sits out too (CERBERUS_DEV_KV_OVERFLOW in pt->status).
  * n_select > 0: every layer attends to that many blocks, chosen per layer and head (needs bounds).  st as in
  * cerberus_ar_step, but st->kv and st->kv_len are not used: the rows are counted in pt->kv_len.  The new row's K and V are
- * attended to at the precision of the computation, as in cerberus_ar_step; the pages keep them in their type, and their bounds
- * if they have any.  max_batch of the context bounds the batch, kv_capacity does not matter.                          */
+ * attended to at the precision of the computation, as in cerberus_ar_step; the pages keep them in their type.  Bounds are
+ * formed when a step fills a page: a part-filled one is its sequence's newest, which every choice takes anyway.  max_batch of the context bounds the batch, kv_capacity does not matter.                          */
 int cerberus_paged_step(cerberus_ctx *ctx, const cerberus_state *st, const cerberus_pages *layers, const cerberus_page_table *pt,
                         int32_t batch, const int32_t *new_rows, int32_t n_select, void *workspace, size_t workspace_bytes,
                         void *stream);

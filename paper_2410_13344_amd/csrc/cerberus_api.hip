@@ -719,24 +719,19 @@ struct PagedStep {
   int n_select;
 };
 
-// Layer l's pages as the QKV projection writes its rows to them.  Where the pages keep bounds it does not: the store that forms
-// them writes the rows.  (A store by itself is 6 us a layer, 5 % of a 7B step of one sequence.)
+// Layer l's pages as the QKV projection writes its rows to them.  (A store by itself is 6 us a layer, 5 % of a 7B step of one sequence.)
 CacheRows page_rows(const Dims& D, const PagedStep& pp, int l) {
   const cerberus_pages& pg = pp.layers[l];
-  return pg.bounds ? CacheRows{} : CacheRows{pg.k, pg.v, (size_t)pg.page_size * D.dh, pp.ws.slot, page_shift_of(pg.page_size)};
+  return CacheRows{pg.k, pg.v, (size_t)pg.page_size * D.dh, pp.ws.slot, page_shift_of(pg.page_size)};
 }
 
-// Layer l's new rows (row b: sequence b) go to their slots, if they are not there yet, then each attends to its sequence's pages
+// Row b of layer l attends to sequence b's pages, its own row among them
 int run_paged_attention(const cerberus_ctx* c, const PagedStep& pp, int l, int batch, hipStream_t s) {
   const Dims& D = c->D;
   const bool bf16 = D.dtype == CERBERUS_BF16;
   const size_t lo = (size_t)c->R64 * D.d;
   const int shift = page_shift_of(pp.pt->page_size);
   const cerberus_pages& pg = pp.layers[l];
-  if (pg.bounds) {
-    const void *k = bf16 ? c->ktree : pp.ws.k_rows, *v = bf16 ? c->vtree : pp.ws.v_rows;
-    HIP_TRY(launch_page_store(PageStoreArgs{pg, k, v, D.d, D.dh, D.d, D.dh, pp.ws.slot, batch, shift, pp.pt->status}, s));
-  }
   if (pp.n_select) {
     PageSelectArgs a{};
     a.pg = pg; a.table = pp.pt->block_table; a.lens = pp.ws.lens; a.max_blocks = pp.pt->max_blocks; a.page_shift = shift;
@@ -784,9 +779,8 @@ int forward_rows(cerberus_ctx* c, const cerberus_state* st, int rows_max, const 
       TRY(run_tile_qkv(c, l, cache, rm.n_rows, rows_max, s));
     } else {
       TRY(run_gemm(c, c->p_qkv[l], rm.n_rows, 0, rows_max, nullptr, 0, s, &pq, qkv_split));
-      const bool rows = pages && D.dtype == CERBERUS_F32;   // (bf16 mode has planes of the new rows anyway)
-      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, cache, rows ? pages->ws.k_rows : c->ktree,
-                             rows ? pages->ws.v_rows : c->vtree, c->ssq, rows_max, s));
+      HIP_TRY(launch_rope_kv(D, rm, pq.out, pq.S, (size_t)pq.out_rows * pq.N, c->rope_cs, c->q, cache, c->ktree, c->vtree,
+                             c->ssq, rows_max, s));
     }
     if (pages) {
       TRY(run_paged_attention(c, *pages, l, sh.batch, s));
@@ -898,6 +892,7 @@ int run_paged_step(cerberus_ctx* c, const cerberus_state* st, const PagedStep& p
   HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, *pp.pt, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
   GemmProb pd{};
   TRY(forward_rows(c, &in_pages, batch, c->tree, AttnShape{1, batch, 0, 0}, &pd, s, &pp));
+  HIP_TRY(launch_page_bounds(pp.layers, D.n_layers, pp.ws.slot, batch, s));
   TRY(run_lm_head(c, pd, nullptr, batch, s));
   HIP_TRY(launch_accept(D, c->tree, c->rm, c->g, c->rm.row_tok, in_pages, c->path, c->last_row, batch, s));
   HIP_TRY(launch_gate(D.d, D.threshold, c->h_last, c->last_row, c->taps.forced_gate_hidden, c->rm.seq_T, batch, st->entropy,

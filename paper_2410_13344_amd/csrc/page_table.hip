@@ -208,11 +208,57 @@ __device__ __forceinline__ float lower(float a, float b) { return (a < b || a !=
 __device__ __forceinline__ float higher(float a, float b) { return (a > b || a != a) ? a : b; }
 }  // namespace
 
+// Lowest and highest coordinates of a page's keys, by a workgroup of 256: a lane folds pieces (16 bytes, always of the same columns)
+// of the rows it sees, then the lanes and the four waves join.
+template <typename T, int DH>
+struct PageFold {
+  static constexpr int N = Vec16<T>::N, LPR = DH / N;                // lanes per row
+  float lo[N], hi[N];
+  __device__ __forceinline__ PageFold() {
+#pragma unroll
+    for (int e = 0; e < N; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+  }
+  __device__ __forceinline__ void add(const uint4& u) {
+    float f[N];
+    Vec16<T>::get(u, f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) { lo[e] = lower(f[e], lo[e]); hi[e] = higher(f[e], hi[e]); }
+  }
+  // to the page's two rows of bounds; sh may still be read by others when this begins
+  __device__ __forceinline__ void write(T* bounds, float (&sh)[2][4][DH]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = threadIdx.x % LPR;
+#pragma unroll
+    for (int off = LPR; off < 64; off <<= 1)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        lo[e] = lower(__shfl_xor(lo[e], off, 64), lo[e]);
+        hi[e] = higher(__shfl_xor(hi[e], off, 64), hi[e]);
+      }
+    __syncthreads();
+    if (lane < LPR) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) { sh[0][wave][piece * N + e] = lo[e]; sh[1][wave][piece * N + e] = hi[e]; }
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * LPR) {
+      const int side = threadIdx.x / LPR;
+      float f[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        f[e] = sh[side][0][piece * N + e];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) f[e] = side ? higher(sh[1][w][piece * N + e], f[e]) : lower(sh[0][w][piece * N + e], f[e]);
+      }
+      *reinterpret_cast<uint4*>(bounds + side * DH + piece * N) = Vec16<T>::put(f);
+    }
+  }
+};
+
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int chunk) {
   constexpr int N = Vec16<T>::N, LPR = DH / N, ROWS = 256 / LPR;   // lanes per row, rows side by side
   __shared__ float sh[2][4][DH];
-  const int h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int h = blockIdx.x, lane = threadIdx.x & 63;
   const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
   const int ps = a.pg.page_size, r_end = (int)min((long long)a.n_rows, (blockIdx.y + 1ll) * chunk);
   const long long slots = (long long)a.pg.n_pages * ps;
@@ -252,15 +298,7 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
       continue;
     }
     const size_t row0 = ((size_t)(s0 >> a.page_shift) * a.pg.n_kv_heads + h) * ps;     // the page's rows of this head
-    float lo[N], hi[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-    auto fold = [&](const uint4& u) {
-      float f[N];
-      Vec16<T>::get(u, f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) { lo[e] = lower(f[e], lo[e]); hi[e] = higher(f[e], hi[e]); }
-    };
+    PageFold<T, DH> fold;
     for (int i = sub; i < len; i += ROWS) {
       uint4 ku = k0, vu = v0;
       if (i > 0) {
@@ -269,35 +307,11 @@ __global__ __launch_bounds__(256) void k_page_store(const PageStoreArgs a, int c
       }
       __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, ku), reinterpret_cast<u32x4_t*>(kp + (row0 + off0 + i) * DH));
       __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, vu), reinterpret_cast<u32x4_t*>(vp + (row0 + off0 + i) * DH));
-      fold(ku);
+      fold.add(ku);
     }
     if (a.pg.bounds) {
-      for (int i = sub; i < off0; i += ROWS) fold(*reinterpret_cast<const uint4*>(kp + (row0 + i) * DH));
-#pragma unroll
-      for (int off = LPR; off < 64; off <<= 1)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          lo[e] = lower(__shfl_xor(lo[e], off, 64), lo[e]);
-          hi[e] = higher(__shfl_xor(hi[e], off, 64), hi[e]);
-        }
-      __syncthreads();                                             // an earlier run's entries have been read
-      if (lane < LPR) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) { sh[0][wave][piece * N + e] = lo[e]; sh[1][wave][piece * N + e] = hi[e]; }
-      }
-      __syncthreads();
-      if (threadIdx.x < 2 * LPR) {
-        const int side = threadIdx.x / LPR;
-        float f[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          f[e] = sh[side][0][piece * N + e];
-#pragma unroll
-          for (int w = 1; w < 4; ++w) f[e] = side ? higher(sh[1][w][piece * N + e], f[e]) : lower(sh[0][w][piece * N + e], f[e]);
-        }
-        T* b = reinterpret_cast<T*>(a.pg.bounds) + ((((size_t)(s0 >> a.page_shift) * a.pg.n_kv_heads + h) * 2 + side) * DH) + piece * N;
-        *reinterpret_cast<uint4*>(b) = Vec16<T>::put(f);
-      }
+      for (int i = sub; i < off0; i += ROWS) fold.add(*reinterpret_cast<const uint4*>(kp + (row0 + i) * DH));
+      fold.write(reinterpret_cast<T*>(a.pg.bounds) + ((size_t)(s0 >> a.page_shift) * a.pg.n_kv_heads + h) * 2 * DH, sh);
     }
     r += len;
   }
@@ -319,6 +333,61 @@ hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s) {
   } else {
     if (wide) hipLaunchKernelGGL((k_page_store<bf16_t, 128>), grid, dim3(256), 0, s, a, chunk);
     else hipLaunchKernelGGL((k_page_store<bf16_t, 64>), grid, dim3(256), 0, s, a, chunk);
+  }
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Bounds after a decoding step, whose rows the projections have written into the pages themselves.  A page that is not full is its sequence's
+// newest, which every choice of blocks takes whatever it scores; so its bounds are formed once, when its last row is there, in one launch
+// for all layers at the end of the step.  16 sequences fill a page every page_size / 16 steps; else the launch finds nothing to do.
+// ---------------------------------------------------------------------------------------------
+namespace {
+constexpr int kBoundsLayers = 64;    // of a launch
+struct PageBoundsArgs {
+  const void* k[kBoundsLayers];
+  void* bounds[kBoundsLayers];
+  const int* slot;
+  int n_kv_heads, page_shift;
+};
+}  // namespace
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_page_bounds(const PageBoundsArgs a) {
+  constexpr int N = Vec16<T>::N, LPR = DH / N, ROWS = 256 / LPR;
+  __shared__ float sh[2][4][DH];
+  const int h = blockIdx.x, l = blockIdx.z, s = a.slot[blockIdx.y], ps = 1 << a.page_shift;
+  if (s < 0 || (s & (ps - 1)) != ps - 1 || !a.bounds[l]) return;
+  const size_t head = (size_t)(s >> a.page_shift) * a.n_kv_heads + h;
+  const T* rows = reinterpret_cast<const T*>(a.k[l]) + head * ps * DH + (threadIdx.x % LPR) * N;
+  PageFold<T, DH> fold;
+  for (int i = threadIdx.x / LPR; i < ps; i += ROWS) fold.add(*reinterpret_cast<const uint4*>(rows + (size_t)i * DH));
+  fold.write(reinterpret_cast<T*>(a.bounds[l]) + head * 2 * DH, sh);
+}
+
+hipError_t launch_page_bounds(const cerberus_pages* layers, int n_layers, const int* slot, int batch, hipStream_t s) {
+  for (int l0 = 0; l0 < n_layers; l0 += kBoundsLayers) {
+    const int n = std::min(kBoundsLayers, n_layers - l0);
+    PageBoundsArgs a{};
+    bool any = false;
+    for (int l = 0; l < n; ++l) {
+      a.k[l] = layers[l0 + l].k;
+      a.bounds[l] = layers[l0 + l].bounds;
+      any = any || a.bounds[l];
+    }
+    if (!any) continue;
+    a.slot = slot;
+    a.n_kv_heads = layers->n_kv_heads;
+    a.page_shift = page_shift_of(layers->page_size);
+    const dim3 grid(layers->n_kv_heads, batch, n);
+    const bool wide = layers->head_dim == 128;
+    if (layers->dtype == CERBERUS_F32) {
+      if (wide) hipLaunchKernelGGL((k_page_bounds<float, 128>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((k_page_bounds<float, 64>), grid, dim3(256), 0, s, a);
+    } else {
+      if (wide) hipLaunchKernelGGL((k_page_bounds<bf16_t, 128>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((k_page_bounds<bf16_t, 64>), grid, dim3(256), 0, s, a);
+    }
   }
   return hipGetLastError();
 }

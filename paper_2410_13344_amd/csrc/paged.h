@@ -21,6 +21,9 @@ struct PageStoreArgs {
 };
 hipError_t launch_page_store(const PageStoreArgs& a, hipStream_t s);
 
+// bounds of the pages that a step's rows (slot [batch], one each) have filled, in all layers that keep any
+hipError_t launch_page_bounds(const cerberus_pages* layers, int n_layers, const int* slot, int batch, hipStream_t s);
+
 struct PageSelectArgs {
   cerberus_pages pg;
   const int *table, *lens;                  // [batch][max_blocks], [batch] rows
@@ -67,7 +70,6 @@ struct PagedWorkspace {
   // of the step over pages
   int *row_start, *first_pos, *slot, *lens; // [batch + 1], [batch], [batch], [batch]
   int* blocks;                              // [batch][n_kv_heads][n_select]
-  void *k_rows, *v_rows;                    // [batch][n_kv_heads][head_dim] (fp32)
   size_t bytes;
 };
 PagedWorkspace paged_workspace(const cerberus_pages& pg, const cerberus_page_table& pt, int batch, int n_heads, int n_select, void* base);

@@ -73,8 +73,6 @@ PagedWorkspace paged_workspace(const cerberus_pages& pg, const cerberus_page_tab
   w.slot = reinterpret_cast<int*>(take((size_t)batch * 4));
   w.lens = reinterpret_cast<int*>(take((size_t)batch * 4));
   w.blocks = reinterpret_cast<int*>(take(row * n_select * 4));
-  w.k_rows = take(pg.dtype == CERBERUS_F32 ? row * pg.head_dim * 4 : 0);
-  w.v_rows = take(pg.dtype == CERBERUS_F32 ? row * pg.head_dim * 4 : 0);
   w.bytes = off;
   return w;
 }

@@ -595,7 +595,7 @@ hipError_t launch_rope_kv(const Dims& D, const RowMap& rm, const float* part, in
   dim3 grid(rows_max, D.nH), block(D.dh / 2);
   if (D.dtype == 0)
     hipLaunchKernelGGL((k_rope_kv<float>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (float*)q, (size_t)0,
-                       cache, (float*)ktree, (float*)vtree, ssq, nb, D);
+                       cache, (float*)nullptr, (float*)nullptr, ssq, nb, D);
   else
     hipLaunchKernelGGL((k_rope_kv<bf16_t>), grid, block, 0, s, part, S, pstride, rope_cs, rm, (bf16_t*)q,
                        (size_t)D.R64 * D.d, cache, (bf16_t*)ktree, (bf16_t*)vtree, ssq, nb, D);

@@ -822,6 +822,34 @@ def test_paged_step_over_chosen_blocks(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+def test_paged_steps_leave_the_bounds_of_full_pages(dtype):
+    """Twenty steps over page ends, blocks chosen: the bounds of every page that a sequence has left behind are its rows', whatever
+    owned the page before, and a choice of the caller's on the same cache goes by them."""
+    pair = _pair(dtype)
+    eng, cfg, lens = pair.engine, pair.cfg, [40, 15, 1]
+    sp = eng.new_state()
+    for b, p in enumerate(_prompts(cfg, lens)):
+        eng.prefill(sp, 3, b, p.to(torch.int32).cuda())
+    cache = B.PageCache(cfg["n_layers"], 14, 16, cfg["n_heads"], cfg["head_dim"], dtype, 3, 8)
+    cache.k.fill_(float("nan"))
+    cache.v.fill_(float("nan"))
+    cache.bounds.fill_(float("nan"))
+    eng.move_prompts(sp, cache, lens)
+    for i in range(20):
+        eng.paged_step(sp, cache, 3, n_select=2 + i % 2)
+    lens = [n + 20 for n in lens]
+    assert cache.kv_len.tolist() == lens and int(cache.status) == 0
+    for l in range(cfg["n_layers"]):
+        for b, n in enumerate(lens):
+            for p in cache.block_table[b, :n // 16].tolist():
+                assert torch.equal(cache.bounds[l, p, :, 0], cache.k[l, p].amin(1)) and torch.equal(cache.bounds[l, p, :, 1], cache.k[l, p].amax(1))
+        q = torch.randn(3, cfg["n_heads"], cfg["head_dim"], device="cuda").to(cache.dtype)
+        for n_select in (1, 2, 3):
+            assert torch.equal(cache.select(l, q, n_select).cpu(), select_plain(q.cpu(), cache.bounds[l].cpu(), cache.block_table.tolist(), lens, n_select, 16, cfg["n_heads"]))
+    pair.engine.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_paged_step_in_a_captured_graph(dtype):
     """Steps captured once and replayed, eager steps in between, against eager steps on another cache."""
     pair = _pair(dtype)
@@ -850,7 +878,7 @@ def test_paged_step_in_a_captured_graph(dtype):
         eng.paged_step(e, ce, 3, rows, n_select=5)
         for n in ("root_token", "cand", "gate_flag", "entropy", "accept_len", "accepted_tokens", "status"):
             assert torch.equal(getattr(a, n), getattr(e, n)), (i, n)
-        assert torch.equal(ca.words, ce.words) and torch.equal(ca.k, ce.k) and torch.equal(ca.v, ce.v) and torch.equal(ca.bounds, ce.bounds)
+        assert torch.equal(ca.words, ce.words) and torch.equal(ca.k, ce.k) and torch.equal(ca.v, ce.v) and torch.equal(ca.bounds, ce.bounds), i
     assert int(ca.status) == 0 and ca.kv_len.tolist() == [111, 15, 51]
     pair.engine.close()
 
