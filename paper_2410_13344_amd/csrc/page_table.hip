@@ -56,13 +56,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
   __shared__ long long back_end[kPlanThreads], row_end[kPlanThreads], need_end[kPlanThreads];
   __shared__ int old_len[kPlanThreads], s_first[kPlanThreads];
   __shared__ long long s_grant;
-  const int t = threadIdx.x, ps = pt.page_size;
+  const int t = threadIdx.x, ps = pt.page_size, shift = 31 - __clz(ps);    // (a power of two)
   const long long cap = (long long)pt.max_blocks * ps;
   int L = 0, n = 0;
   if (t < batch) { L = pt.kv_len[t]; n = min(new_rows ? new_rows[t] : 1, most); }
   const int nf0 = min(max(*pt.n_free, 0), pt.n_pages);
   const bool sane = L >= 0 && L <= cap, ends = n < 0;
-  const int held = sane ? (int)(((long long)L + ps - 1) / ps) : 0;
+  const int held = sane ? (int)(((long long)L + ps - 1) >> shift) : 0;
   const int rows = max(n, 0);
   if (t == 0) s_grant = 0;
 
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
   row_end[t] = re;
   old_len[t] = L;
   const bool fits = t < batch && !ends && sane && (long long)L + rows <= cap && re <= max_rows;
-  const int total = fits ? (int)(((long long)L + rows + ps - 1) / ps) : held;
+  const int total = fits ? (int)(((long long)L + rows + ps - 1) >> shift) : held;
   const int need = fits ? total - held : 0;
   const long long ne = scan_sum(need, sh[2]);
   need_end[t] = ne;
@@ -98,17 +98,17 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
     } else if (item < n_back + grant) {        // a page for a block
       const long long i = item - n_back;
       const int b = owner_of(need_end, batch, i);
-      const long long j = i - (b ? need_end[b - 1] : 0) + ((long long)old_len[b] + ps - 1) / ps;
+      const long long j = i - (b ? need_end[b - 1] : 0) + (((long long)old_len[b] + ps - 1) >> shift);
       pt.block_table[(size_t)b * pt.max_blocks + j] = on_stack(nf1 - 1 - i);
     } else {                                   // a row's slot
       const long long i = item - n_back - grant;
       const int b = owner_of(row_end, batch, i);
       int v = -1;
       if (b < batch && s_first[b] >= 0) {
-        const int pos = s_first[b] + (int)(i - (b ? row_end[b - 1] : 0)), blk = pos / ps;
-        const int have = (int)(((long long)old_len[b] + ps - 1) / ps);
+        const int pos = s_first[b] + (int)(i - (b ? row_end[b - 1] : 0)), blk = pos >> shift;
+        const int have = (int)(((long long)old_len[b] + ps - 1) >> shift);
         const int page = blk < have ? pt.block_table[(size_t)b * pt.max_blocks + blk] : on_stack(nf1 - 1 - ((b ? need_end[b - 1] : 0) + blk - have));
-        v = page * ps + pos % ps;
+        v = page * ps + (pos & (ps - 1));
       }
       slot[i] = v;
     }
@@ -130,17 +130,17 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_plan(const cerberus_page_
 __global__ __launch_bounds__(kPlanThreads) void k_page_commit(const cerberus_page_table pt, const int* __restrict__ new_rows, int most, int batch,
                                                               const int* __restrict__ first_pos) {
   __shared__ long long sh[2][kPlanThreads / 64];
-  const int t = threadIdx.x, ps = pt.page_size;
+  const int t = threadIdx.x, ps = pt.page_size, shift = 31 - __clz(ps);    // (a power of two)
   const long long cap = (long long)pt.max_blocks * ps;
   const int nf0 = min(max(*pt.n_free, 0), pt.n_pages);
   long long back = 0, taken = 0;
   if (t < batch) {
     const int L = pt.kv_len[t], n = min(new_rows ? new_rows[t] : 1, most);
     if (n < 0) {
-      back = L >= 0 && L <= cap ? ((long long)L + ps - 1) / ps : 0;
+      back = L >= 0 && L <= cap ? ((long long)L + ps - 1) >> shift : 0;
       pt.kv_len[t] = 0;
     } else if (n > 0 && first_pos[t] >= 0) {
-      taken = ((long long)L + n + ps - 1) / ps - ((long long)L + ps - 1) / ps;
+      taken = (((long long)L + n + ps - 1) >> shift) - (((long long)L + ps - 1) >> shift);
       pt.kv_len[t] = L + n;
     }
   }

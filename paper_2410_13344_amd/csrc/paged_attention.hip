@@ -32,10 +32,11 @@ __device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int b) {
 // So pieces are not cut below 1024 rows for the last half of them, nor below 512 for the third quarter.  us with per_head pieces for
 // 512 / 1024 / 2048 workgroups without those two limits: 64 sequences of up to 16384 rows x 8 key heads 204 / 192 / 184, one of 131072 91 / 90 / 96,
 // 16 of 257..2049 rows x 32 heads 66 / 63 / 62, lists of 2048 rows for 16 x 8 key heads 31 / 35 / 37.
-__device__ __forceinline__ long long piece_rows(long long total, int per_head) {
-  const int half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
-  const long long a = (total + per_head - 1) / per_head, b = (total + half - 1) / half, c = (total + quarter - 1) / quarter;
-  const long long b1 = b < 1024 ? b : 1024, c1 = c < 512 ? c : 512;
+template <typename I>
+__device__ __forceinline__ I piece_rows(I total, I per_head) {
+  const I half = (per_head + 1) / 2, quarter = (per_head + 3) / 4;
+  const I a = (total + per_head - 1) / per_head, b = (total + half - 1) / half, c = (total + quarter - 1) / quarter;
+  const I b1 = b < 1024 ? b : 1024, c1 = c < 512 ? c : 512;
   return a > b1 ? (a > c1 ? a : c1) : (b1 > c1 ? b1 : c1);
 }
 
@@ -55,7 +56,7 @@ __device__ __forceinline__ Cut find_cut_of(const PagedAttnArgs& a, int item, boo
     total = ((long long)hi << 20) + lo;
   }
   Cut c;
-  const long long want = piece_rows(total, per_head);
+  const long long want = total < 1 << 30 ? piece_rows<unsigned>((unsigned)total, per_head) : piece_rows<long long>(total, per_head);   // (64-bit division is slow)
   c.piece = (int)min((max(want, 1ll) + unit - 1) / unit * unit, (long long)INT_MAX);   // (at INT_MAX nothing is cut)
   const unsigned piece = c.piece;
   int n = 0, cuts = 0;
