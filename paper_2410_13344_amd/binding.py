@@ -350,8 +350,8 @@ class PageCache:
     cerberus_pages of n_layers layers.  max_blocks: blocks of a sequence at most.  The
     bookkeeping (free pages, status, lengths, tables) is one tensor, `words`: a copy of it is a snapshot of who owns which page.
     A call on another stream than torch's current one of the cache's device: pass it as `stream`, and order the streams as for
-    any tensor.  Outputs and workspaces come from torch's allocator per call, on the call's stream, so calls on
-    several streams, and captured graphs, do not share them."""
+    any tensor.  Outputs and workspaces come from torch's allocator, on the call's stream; a workspace serves the calls of one
+    stream, and a captured graph has its own, so calls on several streams, and graphs, do not share them."""
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int, max_seqs: int,
                  max_blocks: int, bounds: bool = True, device="cuda"):
@@ -369,7 +369,7 @@ class PageCache:
             self.device = torch.device("cuda", torch.cuda.current_device())
         device, self._index = self.device, self.device.index
         self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_layers, n_pages, page_size, n_kv_heads, head_dim
-        self.max_seqs, self.max_blocks = max_seqs, max_blocks
+        self.max_seqs, self.max_blocks, self._scale = max_seqs, max_blocks, head_dim ** -0.5
         shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
         self.k = torch.zeros(shape, dtype=self.dtype, device=device)
         self.v = torch.zeros(shape, dtype=self.dtype, device=device)
@@ -387,7 +387,7 @@ class PageCache:
         for i in range(n_layers):
             self.layers[i] = Pages(self.k[i].data_ptr(), self.v[i].data_ptr(), self.bounds[i].data_ptr() if bounds else None,
                                    n_pages, page_size, n_kv_heads, head_dim, dtype)
-        self._bytes = {}
+        self._bytes, self._kept = {}, {}
         self._refs = [C.byref(self.layers[i]) for i in range(n_layers)]      # (what ctypes makes of a struct on every call)
         self._table, self._status = C.byref(self.table), self.status.data_ptr()
 
@@ -407,7 +407,7 @@ class PageCache:
     # A call takes about as long on the host as the smallest kernels run, so the methods below check in few steps, and only a
     # call on a stream of its own, or from another device, pays for torch's context of it.
     def _elsewhere(self, stream) -> bool:
-        return stream is not None or torch.cuda.current_device() != self._index
+        return stream is not None or torch._C._cuda_getDevice() != self._index
 
     def _on(self, stream):
         """Makes the cache's device and the call's stream torch's current ones."""
@@ -417,6 +417,15 @@ class PageCache:
 
     def _stream(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self._index)
+
+    def _workspace(self, nbytes: int, stream: int) -> torch.Tensor:
+        """Of a call on torch's current stream: one per stream, kept, for calls that follow each other there; a graph gets its own."""
+        if torch._C._cuda_isCurrentStreamCapturing():
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        ws = self._kept.get(stream)
+        if ws is None or ws.numel() < nbytes:
+            ws = self._kept[stream] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return ws
 
     def _refuse(self, what: str, t: torch.Tensor, expected) -> None:
         raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}, expected {expected} on {self.device}")
@@ -479,14 +488,14 @@ class PageCache:
         pages, shape = self._layer(layer), (batch, self.n_kv_heads, n_select)
         if not 1 <= n_select <= self.max_blocks:
             raise ValueError(f"n_select {n_select} out of 1..{self.max_blocks}")
-        nbytes = self.workspace_bytes(batch, heads, n_select)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        nbytes, s = self.workspace_bytes(batch, heads, n_select), self._stream()
         if out is None:
-            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            out = self.words.new_empty(shape)
         else:
             self._ints("out", out, shape)
+        ws = self._workspace(nbytes, s)
         _check(lib().cerberus_page_select(pages, self._table, q.data_ptr(), row, batch, heads, n_select, out.data_ptr(), ws.data_ptr(),
-                                          nbytes, self._stream()))
+                                          nbytes, s))
         return out
 
     def attention(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, blocks: Optional[torch.Tensor] = None,
@@ -502,18 +511,17 @@ class PageCache:
             self._ints("blocks", blocks, (batch, self.n_kv_heads, n_select))
             if n_select < 1:
                 raise ValueError("blocks must name at least one block")
-        nbytes = self.workspace_bytes(batch, heads, n_select)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        nbytes, s = self.workspace_bytes(batch, heads, n_select), self._stream()
         if out is None:
-            out = torch.empty((batch, heads, self.head_dim), dtype=self.dtype, device=self.device)
             out_row = heads * self.head_dim
+            out = torch.empty_like(q) if row == out_row else q.new_empty(q.shape)
         else:
             out_batch, out_heads, out_row = self._query("out", out)
             if out_batch != batch or out_heads != heads or (batch > 1 and abs(out_row) < heads * self.head_dim):
                 raise ValueError("out has another shape than q, or rows that overlap")
+        ws = self._workspace(nbytes, s)
         _check(lib().cerberus_paged_attention(pages, self._table, q.data_ptr(), row, out.data_ptr(), out_row, batch, heads,
-                                              self.head_dim ** -0.5 if scale is None else scale, picked, n_select, ws.data_ptr(), nbytes,
-                                              self._stream()))
+                                              self._scale if scale is None else scale, picked, n_select, ws.data_ptr(), nbytes, s))
         return out
 
 
@@ -564,7 +572,7 @@ class Engine:
             cache._ints("new_rows", new_rows, (batch,))
         nbytes = cache.workspace_bytes(batch, self.cfg["n_heads"], n_select)
         with cache._on(stream):
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+            ws = cache._workspace(nbytes, cache._stream())
             cerberus_paged_step(self.ctx, st.struct, cache.layers, cache.table, batch, new_rows, n_select, ws)
 
     def move_prompts(self, st: DeviceState, cache: PageCache, lens: Sequence[int], stream=None) -> PagePlan:

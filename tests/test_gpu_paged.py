@@ -642,6 +642,29 @@ def test_calls_on_two_streams_at_once():
             assert torch.equal(x, alone[i][0]) and torch.equal(y, alone[i][1])
 
 
+def test_graphs_and_eager_calls_do_not_share_a_workspace():
+    """Two graphs captured one after the other, replayed at once on two streams next to eager calls on a third: cut attention of each
+    keeps its own partial results."""
+    caches = [filled(BF16, 8, 2, 64, 16, [20000 + 999 * i, 300], seed=i, poison=False) for i in range(3)]
+    qs = [x[4].cuda() for x in caches]
+    alone = [c.attention(0, q) for (c, *_), q in zip(caches, qs)]
+    graphs, outs = [], []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            outs.append(caches[i][0].attention(0, qs[i]))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    eager = []
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        eager.append(caches[2][0].attention(0, qs[2], stream=streams[2]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(outs[i], alone[i]) for i in range(2)) and all(torch.equal(e, alone[2]) for e in eager)
+
+
 def test_refusals_of_the_binding():
     c = B.PageCache(1, 8, 16, 2, 64, BF16, 3, 4)
     q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
