@@ -143,8 +143,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(const PagedAttnArgs a, in
   const int nkv = a.pg.n_kv_heads, group = a.n_heads / nkv;
   // Workgroups in order of pieces, key heads, tiles of 16 queries; consecutive ones go to the 8 XCDs in turn, so the tiles of
   // one (piece, key head), which read the same rows, are 8 apart and meet in one L2.
-  const long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x, pair = id / (8 * tiles) * 8 + id % 8;
-  const int item = (int)(pair / nkv), hk = (int)(pair % nkv), h0 = (int)(id / 8 % tiles) * 16;   // piece, key head, first of its queries
+  // (Pieces are at most one per sequence and kTarget, heads at most 65535: below 2^31.)
+  const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, of8 = id / 8, pair = of8 / tiles * 8 + id % 8;
+  const int item = pair / nkv, hk = pair % nkv, h0 = of8 % tiles * 16;   // piece, key head, first of its queries
   if (item >= items) return;
   const Cut cut = find_cut(a, item, false, unit, per_head);
   if (cut.b < 0) return;                                            // (uniform over the workgroup)
