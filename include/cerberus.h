@@ -228,7 +228,8 @@ typedef struct {
  * call's other sequences already) and kv_len[b] becomes 0.  row_start (DEVICE [batch + 1]): sequence b's rows are rows
  * row_start[b] .. of the batch, refused ones counted like others (2^31 - 1 where the sum
  * is more).  slot (DEVICE [max_rows]): page * page_size + offset
- * of every row, -1 for rows of refused sequences and behind the last row.  first_pos (DEVICE [batch]): rows that the
+ * of every row, -1 for rows of refused sequences, behind the last row and, with CERBERUS_DEV_BAD_PAGE, where the page number in
+ * the table or among the free pages lies outside the pool.  first_pos (DEVICE [batch]): rows that the
  * sequence held before, -1 where it ended or was refused.  kv_len and the block tables are those with the new rows.
  * A sequence is refused (CERBERUS_DEV_KV_OVERFLOW; it keeps what it has) if its table or max_rows has no room for its
  * rows, or if it needs pages and those that it and the sequences before it need are more than there are: first come,

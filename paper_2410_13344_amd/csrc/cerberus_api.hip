@@ -889,7 +889,7 @@ int run_paged_step(cerberus_ctx* c, const cerberus_state* st, const PagedStep& p
   in_pages.kv = nullptr;
   in_pages.kv_len = pp.pt->kv_len;          // (the acceptance writes the length that the plan has put there already)
   HIP_TRY(launch_page_plan(*pp.pt, new_rows, 1, batch, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, s));
-  HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, *pp.pt, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
+  HIP_TRY(launch_assemble_pages(D, c->rm, in_pages, c->taps, batch, pp.ws.row_start, pp.ws.first_pos, pp.ws.slot, pp.ws.lens, s));
   GemmProb pd{};
   TRY(forward_rows(c, &in_pages, batch, c->tree, AttnShape{1, batch, 0, 0}, &pd, s, &pp));
   HIP_TRY(launch_page_bounds(pp.layers, D.n_layers, pp.ws.slot, batch, s));

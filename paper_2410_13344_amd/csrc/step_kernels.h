@@ -43,7 +43,7 @@ hipError_t launch_assemble(const Dims& D, const TreeDev& tr, const RowMap& rm, c
                            const cerberus_taps& tp, int batch, int mode, const PromptArgs& pa, const AttnPlanCfg& ap, hipStream_t s);
 // rows of a step over pages, from what the plan of its rows left; lens [batch]: rows every sequence attends to
 hipError_t launch_assemble_pages(const Dims& D, const RowMap& rm, const cerberus_state& st, const cerberus_taps& tp, int batch,
-                                 const cerberus_page_table& pt, const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s);
+                                 const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s);
 // after the layers of a prompt pass: commits the rows; in the last pass the row map becomes that of the tail rows
 hipError_t launch_prompt_commit(const RowMap& rm, const cerberus_state& st, int* last_row, int batch, int seq, int last_pass,
                                 hipStream_t s);

@@ -216,18 +216,13 @@ hipError_t launch_assemble(const Dims& D, const TreeDev& tr, const RowMap& rm, c
 // out has a row nobody looks at (token 0, no slot, nothing to attend to, outside the taps).  slot: of the packed rows in, of the
 // sequences out.
 __global__ __launch_bounds__(64) void k_assemble_pages(const Dims D, const RowMap rm, const cerberus_state st, const cerberus_taps tp,
-                                                       int batch, const cerberus_page_table pt, const int* row_start, const int* first_pos,
-                                                       int* slot, int* lens) {
+                                                       int batch, const int* row_start, const int* first_pos, int* slot, int* lens) {
   const int b = threadIdx.x;
   bool runs = false;
   int own = -1;
   if (b < batch) {
     runs = first_pos[b] >= 0 && row_start[b + 1] > row_start[b];
-    if (runs) own = slot[row_start[b]];
-    if (runs && (own < 0 || own / pt.page_size >= pt.n_pages)) {   // (a page number that no pool has)
-      atomicOr(pt.status, (int)CERBERUS_DEV_BAD_PAGE);
-      own = -1;
-    }
+    if (runs) own = slot[row_start[b]];     // (-1 where the page is none of the pool's: the plan has reported it)
   }
   __syncthreads();                          // every packed slot has been read
   if (b == 0) *rm.n_rows = batch;
@@ -248,9 +243,9 @@ __global__ __launch_bounds__(64) void k_assemble_pages(const Dims D, const RowMa
 }
 
 hipError_t launch_assemble_pages(const Dims& D, const RowMap& rm, const cerberus_state& st, const cerberus_taps& tp, int batch,
-                                 const cerberus_page_table& pt, const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s) {
+                                 const int* row_start, const int* first_pos, int* slot, int* lens, hipStream_t s) {
   static_assert(CERBERUS_MAX_BATCH <= 64, "a thread per sequence, one wave");
-  hipLaunchKernelGGL(k_assemble_pages, dim3(1), dim3(64), 0, s, D, rm, st, tp, batch, pt, row_start, first_pos, slot, lens);
+  hipLaunchKernelGGL(k_assemble_pages, dim3(1), dim3(64), 0, s, D, rm, st, tp, batch, row_start, first_pos, slot, lens);
   return hipGetLastError();
 }
 
