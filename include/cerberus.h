@@ -258,7 +258,8 @@ size_t cerberus_paged_workspace_bytes(const cerberus_pages *pg, const cerberus_p
  * a key head, block j scores sum_d Q_d * (Q_d >= 0 ? highest_d : lowest_d), no less than the sum of its group's scores on any
  * one key of the block.  Per sequence and key head the newest block, then the first one, then those with the highest scores
  * (summed in 64 bits; NaN counts as the highest; ties: the lower index) up to n_select are written to blocks (DEVICE
- * [batch][n_kv_heads][n_select]) in ascending order, the rest -1.  Needs pg->bounds.            */
+ * [batch][n_kv_heads][n_select]) in ascending order, the rest -1.  Among those that go by their scores, blocks whose page
+ * number lies outside the pool come last; the choice does not report them, the attention does.  Needs pg->bounds.           */
 int cerberus_page_select(const cerberus_pages *pg, const cerberus_page_table *pt, const void *q, int64_t q_row_stride,
                          int32_t batch, int32_t n_heads, int32_t n_select, int32_t *blocks, void *workspace,
                          size_t workspace_bytes, void *stream);

@@ -7,7 +7,9 @@ namespace cerb {
 
 namespace {
 
-// Order of a score as an unsigned number: higher score, higher number, none is 0; NaN counts as +inf, both zeros alike.
+constexpr unsigned long long kOutside = 1;   // number of a block whose page the pool does not have: below that of every score
+
+// Order of a score as an unsigned number: higher score, higher number, none below 2; NaN counts as +inf, both zeros alike.
 __device__ __forceinline__ unsigned long long order_of(double s) {
   if (s != s) s = INFINITY;
   const long long b = __double_as_longlong(s + 0.0);
@@ -32,7 +34,7 @@ template <> struct Piece<bf16_t> {
 // ---------------------------------------------------------------------------------------------
 // Scores.  With Q the sum of a key head's queries, the block's score is the sum over d of Q_d times the higher bound where Q_d >= 0
 // and the lower one elsewhere.  Two blocks next to the border of the choice change places with the last bits of a sum, so
-// products and sums are in 64 bits, where the products of 16- or 24-bit numbers are exact.  A wave takes 32 or 64 blocks of one
+// products and sums are in 64 bits, where the products of 16- or 24-bit numbers are exact.  A wave takes 16, 32 or 64 blocks of one
 // key head at a time.  Each of LPB lanes per block loads 16 bytes of both sides, the same columns for every block; a mask
 // from its queries' signs takes one side's bits before anything is computed (an infinite bound that does not count is
 // not a NaN).  Eight blocks per lane are in flight; their sums over the lanes are folded together, eight values over 2, 4, 8 lanes,
@@ -87,12 +89,11 @@ struct Scores {
     const int lane = threadIdx.x & 63;
     double s[8];
     uint4 lo[8], hi[8];
-    int pg[8];
+    page = page < n_pages ? page : -1;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      pg[i] = __shfl(page, i * BPL + lane / LPB, 64);
-      if (pg[i] >= n_pages) pg[i] = -1;
-      const T* p = bounds + (size_t)max(pg[i], 0) * page_stride;
+      const int pg = max(__shfl(page, i * BPL + lane / LPB, 64), 0);       // (page 0 where there is none: what it gives is not used)
+      const T* p = bounds + (size_t)pg * page_stride;
       lo[i] = *reinterpret_cast<const uint4*>(p);
       hi[i] = *reinterpret_cast<const uint4*>(p + DH);
     }
@@ -106,7 +107,6 @@ struct Scores {
       s[i] = 0.0;
 #pragma unroll
       for (int e = 0; e < N; ++e) s[i] = fma(q[e], (double)Piece<T>::get(x, e), s[i]);
-      if (pg[i] < 0) s[i] = 0.0;
     }
     // fold: lanes whose bit is set go on with the upper half of the values
 #pragma unroll
@@ -119,10 +119,10 @@ struct Scores {
       }
 #pragma unroll
     for (int bit = LPB / 16; bit >= 1; bit >>= 1) s[0] += __shfl_xor(s[0], bit, 64);
-    if (sub % (LPB / 8) == 0) {
-      const int j = j0 + sub / (LPB / 8) * BPL + lane / LPB;             // which of the eight: the top three bits of sub
-      if (j < held) put(j, j == 0 || j == held - 1 ? 0 : order_of(s[0]));   // (those two go by their places)
-    }
+    const int at = sub / (LPB / 8) * BPL + lane / LPB, j = j0 + at;       // which of the eight: the top three bits of sub
+    const bool outside = __shfl(page, at, 64) < 0;
+    if (sub % (LPB / 8) == 0 && j < held)
+      put(j, j == 0 || j == held - 1 ? 0 : outside ? kOutside : order_of(s[0]));   // (those two go by their places)
   }
 };
 

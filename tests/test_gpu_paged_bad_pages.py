@@ -59,3 +59,41 @@ def test_paged_step_writes_nothing_for_a_page_number_that_passes_32_bits(dtype):
             assert torch.equal(now, before), bad
         assert torch.equal(cache.bounds, kept[2])
     eng.close()
+
+
+# ------------------------------------------------------------------------------------------------
+# the choice of blocks
+# ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("blocks", [12, 1500])                   # scored and picked in one launch, in two
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_select_takes_blocks_outside_the_pool_after_all_others(dtype, blocks):
+    """Scores below zero, one of -inf, one a tie: every block of a page that is there goes before those of pages that are not; the
+    newest and the first go by their places."""
+    page, dh, held = 16, 64, 12
+    c = B.PageCache(1, held, page, 2, dh, dtype, 2, blocks)
+    c.block_table[:, :held] = torch.arange(held, dtype=torch.int32, device="cuda")
+    c.block_table[1, 0] = held                                   # the first one's page is not there either
+    for b in range(2):
+        c.block_table[b, 4], c.block_table[b, 7], c.block_table[b, 9] = held, -3, 2 ** 31 - 1
+    c.kv_len.fill_(held * page - 5)
+    for j in range(held):                                        # block j scores -(j % 4 + 1) * 64 * 4, block 5 -inf
+        c.bounds[0, j] = -(j % 4 + 1.0)
+    c.bounds[0, 5] = float("-inf")
+    q = torch.ones(2, 8, dh, dtype=c.dtype, device="cuda")       # groups of four queries
+    there = [8, 1, 2, 6, 10, 3, 5]                               # by score, then place; 0 and 11 go first
+    for n in range(1, held + 1):
+        got = c.select(0, q, n).cpu()
+        best = ([11, 0] + there + [4, 7, 9])[:n]
+        want = torch.tensor(sorted(best), dtype=torch.int32).expand(2, 2, n)
+        assert torch.equal(got, want), (n, got.tolist())
+
+
+def test_select_among_nothing_but_pages_outside_the_pool():
+    for blocks in (9, 1100):
+        c = B.PageCache(1, 4, 16, 1, 64, BF16, 1, blocks)
+        c.block_table.fill_(77)
+        c.kv_len.fill_(9 * 16)
+        q = torch.ones(1, 1, 64, dtype=c.dtype, device="cuda")
+        for n in (1, 2, 5, 8, 9):
+            assert c.select(0, q, n)[0, 0].tolist() == ([8] if n == 1 else list(range(n - 1)) + [8])
