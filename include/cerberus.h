@@ -249,7 +249,8 @@ int cerberus_page_store(const cerberus_pages *pg, const void *k, int64_t k_row_s
 
 /* Bytes of DEVICE workspace (256-byte aligned) that cerberus_page_select, cerberus_paged_attention or, with the pages of a
  * context's layers, cerberus_paged_step need for such a call; 0 on bad input.  n_select 0: no selection.  Calls that share
- * a workspace must not overlap.                                                                 */
+ * a workspace must not overlap, nor be made by two host threads at once, on one stream either: a call can be more than one launch.
+ * The same holds for plans and steps that share a page table.                                   */
 size_t cerberus_paged_workspace_bytes(const cerberus_pages *pg, const cerberus_page_table *pt, int32_t batch, int32_t n_heads,
                                       int32_t n_select);
 

@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -351,7 +352,8 @@ class PageCache:
     bookkeeping (free pages, status, lengths, tables) is one tensor, `words`: a copy of it is a snapshot of who owns which page.
     A call on another stream than torch's current one of the cache's device: pass it as `stream`, and order the streams as for
     any tensor.  Outputs and workspaces come from torch's allocator, on the call's stream; a workspace serves the calls of one
-    stream, and a captured graph has its own, so calls on several streams, and graphs, do not share them."""
+    stream, and a captured graph has its own, so calls on several streams, and graphs, do not share them.  Several threads may
+    call: the launches of a call are enqueued together, never between those of another call on the same cache."""
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: int, max_seqs: int,
                  max_blocks: int, bounds: bool = True, device="cuda"):
@@ -388,6 +390,9 @@ class PageCache:
             self.layers[i] = Pages(self.k[i].data_ptr(), self.v[i].data_ptr(), self.bounds[i].data_ptr() if bounds else None,
                                    n_pages, page_size, n_kv_heads, head_dim, dtype)
         self._bytes, self._kept = {}, {}
+        # ctypes lets other threads run during a call; one that is two launches (a plan, a cut attention, a long choice), or hands its
+        # workspace on to the next on its stream, must not have another one's launches between its own
+        self._enqueue = threading.RLock()
         self._refs = [C.byref(self.layers[i]) for i in range(n_layers)]      # (what ctypes makes of a struct on every call)
         self._table, self._status = C.byref(self.table), self.status.data_ptr()
 
@@ -452,7 +457,8 @@ class PageCache:
             out = PagePlan(batch, max_rows, self.device)
         elif out.batch != batch or out.device != self.device or (max_rows is not None and max_rows != out.max_rows):
             raise ValueError("out is a plan of another batch, device or max_rows")
-        _check(lib().cerberus_page_plan(self._table, new_rows.data_ptr(), batch, out.max_rows, *out.pointers, self._stream()))
+        with self._enqueue:
+            _check(lib().cerberus_page_plan(self._table, new_rows.data_ptr(), batch, out.max_rows, *out.pointers, self._stream()))
         return out
 
     def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, stream=None) -> None:
@@ -493,9 +499,10 @@ class PageCache:
             out = self.words.new_empty(shape)
         else:
             self._ints("out", out, shape)
-        ws = self._workspace(nbytes, s)
-        _check(lib().cerberus_page_select(pages, self._table, q.data_ptr(), row, batch, heads, n_select, out.data_ptr(), ws.data_ptr(),
-                                          nbytes, s))
+        with self._enqueue:
+            ws = self._workspace(nbytes, s)
+            _check(lib().cerberus_page_select(pages, self._table, q.data_ptr(), row, batch, heads, n_select, out.data_ptr(),
+                                              ws.data_ptr(), nbytes, s))
         return out
 
     def attention(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, blocks: Optional[torch.Tensor] = None,
@@ -519,9 +526,10 @@ class PageCache:
             out_batch, out_heads, out_row = self._query("out", out)
             if out_batch != batch or out_heads != heads or (batch > 1 and abs(out_row) < heads * self.head_dim):
                 raise ValueError("out has another shape than q, or rows that overlap")
-        ws = self._workspace(nbytes, s)
-        _check(lib().cerberus_paged_attention(pages, self._table, q.data_ptr(), row, out.data_ptr(), out_row, batch, heads,
-                                              self._scale if scale is None else scale, picked, n_select, ws.data_ptr(), nbytes, s))
+        with self._enqueue:
+            ws = self._workspace(nbytes, s)
+            _check(lib().cerberus_paged_attention(pages, self._table, q.data_ptr(), row, out.data_ptr(), out_row, batch, heads,
+                                                  self._scale if scale is None else scale, picked, n_select, ws.data_ptr(), nbytes, s))
         return out
 
 
@@ -571,7 +579,7 @@ class Engine:
         if new_rows is not None:
             cache._ints("new_rows", new_rows, (batch,))
         nbytes = cache.workspace_bytes(batch, self.cfg["n_heads"], n_select)
-        with cache._on(stream):
+        with cache._on(stream), cache._enqueue:
             ws = cache._workspace(nbytes, cache._stream())
             cerberus_paged_step(self.ctx, st.struct, cache.layers, cache.table, batch, new_rows, n_select, ws)
 
