@@ -235,16 +235,34 @@ def cerberus_accept_noalloc(ctx: int, node_argmax: torch.Tensor, node_token: tor
                                          _stream_ptr(stream)))
 
 
+# The calls over pages take sizes and strides from their tensors; what the kernels would read or write past a tensor's end, or take for
+# another type, is refused here.
+
+def _page_ints(t: torch.Tensor, *shape: int) -> bool:
+    return t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape
+
+
+def _page_rows(t: torch.Tensor, pages: Pages, heads: int, dense: bool) -> bool:
+    """[rows][heads][head_dim] of the pages' type, a row's heads one after the other if `dense`."""
+    return (t.is_cuda and t.dtype == (torch.float32 if pages.dtype == CERBERUS_F32 else torch.bfloat16) and t.dim() == 3 and
+            t.shape[1] == heads and t.shape[2] == pages.head_dim and t.stride(2) == 1 and
+            (not dense or heads == 1 or t.stride(1) == pages.head_dim))
+
+
 def cerberus_page_plan(table: PageTable, new_rows: torch.Tensor, max_rows: int, row_start: torch.Tensor, first_pos: torch.Tensor,
                        slot: torch.Tensor, stream=None) -> None:
-    assert all(t.is_cuda and t.dtype == torch.int32 for t in (new_rows, row_start, first_pos, slot))
-    _check(lib().cerberus_page_plan(table, new_rows.data_ptr(), new_rows.shape[0], max_rows, row_start.data_ptr(),
-                                    first_pos.data_ptr(), slot.data_ptr(), _stream_ptr(stream)))
+    assert all(t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() for t in (new_rows, row_start, first_pos, slot))
+    batch = new_rows.shape[0]
+    assert row_start.shape[0] > batch and first_pos.shape[0] >= batch and slot.shape[0] >= max_rows
+    _check(lib().cerberus_page_plan(table, new_rows.data_ptr(), batch, max_rows, row_start.data_ptr(), first_pos.data_ptr(),
+                                    slot.data_ptr(), _stream_ptr(stream)))
 
 
 def cerberus_page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, status: Optional[torch.Tensor] = None,
                         stream=None) -> None:
-    assert k.is_cuda and v.is_cuda and slot.is_cuda and slot.dtype == torch.int32 and k.shape == v.shape and k.shape[0] == slot.shape[0]
+    assert _page_ints(slot, slot.shape[0]) and k.shape[0] == v.shape[0] == slot.shape[0]
+    assert _page_rows(k, pages, pages.n_kv_heads, False) and _page_rows(v, pages, pages.n_kv_heads, False)
+    assert status is None or (status.is_cuda and status.dtype == torch.int32 and status.numel() >= 1)
     _check(lib().cerberus_page_store(pages, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                                      slot.data_ptr(), slot.shape[0], _ptr(status), _stream_ptr(stream)))
 
@@ -255,14 +273,17 @@ def cerberus_paged_workspace_bytes(pages: Pages, table: PageTable, batch: int, n
 
 def cerberus_page_select(pages: Pages, table: PageTable, q: torch.Tensor, blocks: torch.Tensor, workspace: torch.Tensor,
                          stream=None) -> None:
-    assert q.is_cuda and workspace.is_cuda and blocks.is_cuda and blocks.dtype == torch.int32 and blocks.shape[0] == q.shape[0]
+    assert workspace.is_cuda and workspace.is_contiguous() and _page_rows(q, pages, q.shape[1], True)
+    assert _page_ints(blocks, q.shape[0], pages.n_kv_heads, blocks.shape[-1])
     _check(lib().cerberus_page_select(pages, table, q.data_ptr(), q.stride(0), q.shape[0], q.shape[1], blocks.shape[2],
                                       blocks.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
 
 
 def cerberus_paged_attention(pages: Pages, table: PageTable, q: torch.Tensor, out: torch.Tensor, scale: float,
                              blocks: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
-    assert q.is_cuda and out.is_cuda and workspace.is_cuda and out.shape == q.shape and (blocks is None or blocks.is_cuda)
+    assert workspace.is_cuda and workspace.is_contiguous()
+    assert out.shape == q.shape and _page_rows(q, pages, q.shape[1], True) and _page_rows(out, pages, q.shape[1], True)
+    assert blocks is None or _page_ints(blocks, q.shape[0], pages.n_kv_heads, blocks.shape[-1])
     _check(lib().cerberus_paged_attention(pages, table, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), q.shape[0], q.shape[1],
                                           scale, _ptr(blocks), 0 if blocks is None else blocks.shape[2], workspace.data_ptr(),
                                           workspace.numel(), _stream_ptr(stream)))
@@ -270,7 +291,8 @@ def cerberus_paged_attention(pages: Pages, table: PageTable, q: torch.Tensor, ou
 
 def cerberus_paged_step(ctx: int, state: State, layers, table: PageTable, batch: int, new_rows: Optional[torch.Tensor], n_select: int,
                         workspace: torch.Tensor, stream=None) -> None:
-    assert workspace.is_cuda and (new_rows is None or (new_rows.is_cuda and new_rows.dtype == torch.int32))
+    assert workspace.is_cuda and workspace.is_contiguous()
+    assert new_rows is None or (_page_ints(new_rows, new_rows.shape[0]) and new_rows.shape[0] >= batch)
     _check(lib().cerberus_paged_step(ctx, C.byref(state), layers, table, batch, _ptr(new_rows), n_select, workspace.data_ptr(),
                                      workspace.numel(), _stream_ptr(stream)))
 
