@@ -269,8 +269,8 @@ int cerberus_page_select(const cerberus_pages *pg, const cerberus_page_table *pt
  * stored already), out laid out like q with a row stride of its own.  With blocks (as cerberus_page_select writes them, in any order; an index twice counts
  * twice; indexes outside 0..blocks held - 1 are no block) each key head reads those blocks only.  Where there is no row to
  * read, or every score is -inf, the output is zero.  What lies in a page behind the last row is never used.  A kv_len above what the table holds
- * counts as that, a page number outside the pool as no rows (CERBERUS_DEV_BAD_PAGE, pt->status).  fp32 softmax and sums; bf16
- * probabilities are two bf16 planes.                                                            */
+ * counts as that, a page number outside the pool as no rows (CERBERUS_DEV_BAD_PAGE, pt->status).  scale: finite, below
+ * 2.35e38 either side of zero.  fp32 softmax and sums; bf16 probabilities are two bf16 planes.  */
 int cerberus_paged_attention(const cerberus_pages *pg, const cerberus_page_table *pt, const void *q, int64_t q_row_stride,
                              void *out, int64_t out_row_stride, int32_t batch, int32_t n_heads, float scale,
                              const int32_t *blocks, int32_t n_select, void *workspace, size_t workspace_bytes, void *stream);

@@ -160,7 +160,8 @@ int cerberus_paged_attention(const cerberus_pages* pg, const cerberus_page_table
   TRY(check_same_pages(pg, pt));
   TRY(check_heads(pg, n_heads));
   if (blocks ? n_select < 1 : n_select != 0) return set_error(CERBERUS_ERR_ARG, "blocks and n_select go together");
-  if (!std::isfinite(scale)) return set_error(CERBERUS_ERR_ARG, "scale must be finite");
+  // (the kernel's scores are in powers of two: with a factor that is infinite there, scores of zero would be NaN)
+  if (!std::isfinite(scale * 1.44269504088896340736f)) return set_error(CERBERUS_ERR_ARG, "scale must be finite, and scale / ln 2 too");
   TRY(check_rows(pg, q, q_row_stride, "q"));
   TRY(check_rows(pg, out, out_row_stride, "out"));
   TRY(check_workspace(pg, pt, batch, n_heads, n_select, workspace, workspace_bytes));

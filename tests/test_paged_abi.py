@@ -123,6 +123,12 @@ def test_select_and_attention_arguments(L):
     refused(L, ARG, attend(scale=float("inf")), "scale")
 
 
+@pytest.mark.parametrize("scale", [2.4e38, -2.4e38, 3.4e38, float("-inf")])
+def test_a_scale_whose_power_of_two_is_infinite_is_refused(L, scale):
+    """Scores are formed in powers of two, scale / ln 2 = 1.4427 scale: from 2.36e38 on that is no float."""
+    refused(L, ARG, L.cerberus_paged_attention(pages(), table(), A, 256, A, 256, 2, 4, scale, None, 0, A, 1 << 30, None), "scale")
+
+
 def test_workspace_follows_the_work_not_the_table(L):
     """A wide table or a large batch asks for no more partial results than the card has workgroups for."""
     pg = pages(n_kv_heads=8, head_dim=128, n_pages=1 << 20)
