@@ -268,7 +268,8 @@ int cerberus_page_select(const cerberus_pages *pg, const cerberus_page_table *pt
 /* Attention of one new token per sequence: out = softmax(scale * q K^T) V over rows 0..kv_len[b]-1 (the token's own row is
  * stored already), out laid out like q with a row stride of its own.  With blocks (as cerberus_page_select writes them, in any order; an index twice counts
  * twice; indexes outside 0..blocks held - 1 are no block) each key head reads those blocks only.  Where there is no row to
- * read, or every score is -inf, the output is zero.  What lies in a page behind the last row is never used.  A kv_len above what the table holds
+ * read, or every score is -inf, the output is zero.  What lies in a page behind the last row is never used; a value that is infinite or NaN in
+ * a row that is read makes its column infinite or NaN (NaN also where a probability of 0, or a plane of one, meets it).  A kv_len above what the table holds
  * counts as that, a page number outside the pool as no rows (CERBERUS_DEV_BAD_PAGE, pt->status).  scale: finite, below
  * 2.35e38 either side of zero.  fp32 softmax and sums; bf16 probabilities are two bf16 planes.  */
 int cerberus_paged_attention(const cerberus_pages *pg, const cerberus_page_table *pt, const void *q, int64_t q_row_stride,
