@@ -232,9 +232,10 @@ __device__ __forceinline__ void pick(int held, int n_select, Number number, int*
 // (512 threads: 13.2 us for 128 lists of 512 blocks, 7.8 for 256 of up to 208; 1024: 16.3 and 9.4, 256: 14.7 and 8.4)
 constexpr int kOneLaunch = 1024, kChooseThreads = 512, kChooseWaves = kChooseThreads / 64;
 
-// Up to kOneLaunch blocks: a workgroup per (sequence, key head) scores them all into LDS, one of its waves picks.  13.1 us for 32 of
+// Up to kOneLaunch blocks: a workgroup per (sequence, key head) scores them all into LDS, one of its waves picks.  12.8 us for 32 of
 // 512 blocks of 16 sequences x 8 key heads (33 MB of bounds; without the pick 9.8, without the scores 4.8), of which 2.4 are
-// the launch, and a scan of 128 lists keeps half the compute units busy.  Two launches, as below, took 22.5.
+// the launch, and a scan of 128 lists keeps half the compute units busy.  us of 8 blocks chosen, this launch / the two below: 128 lists of 64 blocks
+// 6.8 / 22, of 512 13.9 / 28, of 1024 24 / 32; 512 lists of 1024 51 / 72; only few long lists lose (8 of 1024: 20.6 / 17.8).
 template <typename T, int DH>
 __global__ __launch_bounds__(kChooseThreads) void k_page_choose(const PageSelectArgs a) {
   __shared__ unsigned long long keys[kOneLaunch];

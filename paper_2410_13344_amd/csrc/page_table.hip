@@ -156,6 +156,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_page_commit(const cerberus_pag
   *pt.n_free = (int)(min((long long)pt.n_pages, nf0 + back) - taken);
 }
 
+// us, one workgroup / many, for plans of 16, 1024, 2048, 4096 and 8192 rows: of one prompt 3.5 / 6.6, 4.3 / 6.6, 4.7 / 6.9, 5.7 / 6.9, 8.0 / 6.9; of 256
+// sequences 6.3 / 8.8, 8.1 / 9.8, 9.0 / 10.0, 10.8 / 10.1, 15.0 / 10.1.  (What comes back from sequences that end is not in the rule: 1024 of 512 pages each
+// take one workgroup 0.53 ms.)
 constexpr int kRowsOfOne = 2048, kPlanWorkgroups = 128;
 
 hipError_t launch_page_plan(const cerberus_page_table& pt, const int* new_rows, int most, int batch, int max_rows, int* row_start,

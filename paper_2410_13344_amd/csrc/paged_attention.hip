@@ -127,9 +127,9 @@ template <int DH> struct Stage<float, DH> {
 // A lane's outputs all belong to its query, so the running maximum's factor is the lane's own.
 // bf16: probabilities go into the second product as two bf16 planes (p to 2^-17): the matrix units have time.
 // Two waves per SIMD with 256 registers each: 16 KB of K and V in work and 16 KB in flight per wave, 128 KB in flight per compute unit.
-// Measured (bf16, 128 columns, this kernel alone): 131072 rows x 8 key heads 81-92 us, 5.8-6.6 TB/s with the matrix units busy 6 % of the time; 64
-// sequences of up to 16384 rows x 8 key heads 180, 6.1; 16 of 257..2049 x 32 heads 54, 6.0; 1025 rows x 32 heads 6.6, which
-// is the chain of length, table, rows and join.  A copy of 1 GiB runs at 5.1 TB/s.
+// Measured (bf16, 128 columns, this kernel alone, least and average of 421 launches): 131072 rows x 8 key heads 81-84 us, 6.4-6.7 TB/s with the matrix
+// units busy 6 % of the time; 64 sequences of up to 16384 rows x 8 key heads 176-184, 6.0-6.2; 16 of 257..2049 x 32 heads 55-58,
+// 5.6-5.8; 1025 rows x 32 heads 5.6-7.2, which is the chain of length, table and rows.  A copy of 1 GiB runs at 5.1 TB/s.
 // STEP: a decoding step's queries and outputs are two bf16 planes, and the newest row has a second plane next to the cache.
 // ---------------------------------------------------------------------------------------------
 // ONCE: K and V are read once in the launch (up to 16 queries per key head): loaded with the streaming hint.  A model's layers hold more
@@ -504,7 +504,10 @@ namespace {
 
 constexpr int kTarget = 2048;     // workgroups a launch aims for at most
 constexpr int kTurns = 4;         // turns of a workgroup that take less time than a join
-constexpr int kLists = 256;       // workgroups that keep the memory busy: 128 lists of 2048 rows take 38.3 us whole, 31.8 cut and joined
+// Lists of chosen blocks from which on none is cut: a workgroup for every compute unit.  us, whole / cut and joined, for 128, 192, 256, 320, 512, 640 and 1024
+// lists of 2048 rows: 38 / 29, 39 / 39, 43 / 50, 70 / 64, 82 / 86, 114 / 111, 161 / 171; of 8192 rows: 142 / 91, 139 / 129, 162 / 171, 273 / 220, 320 / 329,
+// 456 / 462, 644 / 656.  Just above a whole number of rounds (257..383 and 513..639 lists) long lists would still be better cut.
+constexpr int kLists = 256;
 
 int head_tiles(int n_heads, int n_kv_heads) { return (n_heads / n_kv_heads + 15) / 16; }
 // pieces that a launch aims for per (key head, 16 queries)
